@@ -9,6 +9,7 @@
 
 #include "../../include/petals_client.h"
 #include "../../include/petals_span.h"
+#include "client_internal.h"
 #include "common.h"
 #include "host_util.h"
 #include "rowops.h"
@@ -1194,6 +1195,14 @@ int check_client_config(const petals_client_config *c) {
     return PETALS_OK;
 }
 }  // namespace
+
+ps_client_view ps_view(const petals_client *c) {
+    size_t bytes = 0;
+    petals_client_workspace_bytes(&c->cfg, &bytes);
+    return ps_client_view{&c->cfg, &c->p, (uint8_t *)c->a, bytes};      // a is the first thing in it
+}
+
+int ps_check_client_config(const petals_client_config *cfg) { return check_client_config(cfg); }
 
 extern "C" {
 

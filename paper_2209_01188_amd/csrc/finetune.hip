@@ -1,0 +1,491 @@
+// Scoring and the client's ends of a fine-tuning step: log probabilities, distillation loss with its gradient, gradient of
+// the embedding lookup.  (The LM head's backward product is in head_backward.hip.)
+#include <math.h>
+
+#include "../../include/petals_finetune.h"
+#include "../../include/petals_span.h"
+#include "client_internal.h"
+#include "common.h"
+#include "host_util.h"
+#include "ln_backward.h"
+
+namespace {
+
+// ------------------------------------------------------------------------------------ a row's softmax statistics
+//
+// One pass over the row: every thread keeps the maximum m of what it has seen, S = sum of e^t and D = sum of t e^t with
+// t = (l - m) / T, and rescales the two when m grows.  The exponentials are fp32 (base 2: x = t log2(e), D in that unit as
+// well); the sums are fp64, so that S - 1, what is left beside the largest token, keeps its digits where that token has
+// nearly everything: log S and -D / S are the two parts of the entropy, both >= 0, and nothing cancels between them.
+constexpr double LN2 = 0.69314718055994530942;
+
+struct RowStat {
+    float m;
+    double S, D;
+};
+__device__ __forceinline__ RowStat merge(const RowStat &a, const RowStat &b, double invT) {
+    const float m = fmaxf(a.m, b.m);
+    if (m == -INFINITY) return RowStat{m, a.S + b.S, a.D + b.D};        // (sums of nothing, or NaN)
+    const double ta = ((double)a.m - m) * invT, tb = ((double)b.m - m) * invT, ea = exp_f64(ta), eb = exp_f64(tb);
+    // a part without any logit above -infinity: S = D = 0, and its t is no number to multiply with
+    const double da = a.m == -INFINITY ? 0.0 : ea * fma(ta / LN2, a.S, a.D), db = b.m == -INFINITY ? 0.0 : eb * fma(tb / LN2, b.S, b.D);
+    return RowStat{m, ea * a.S + eb * b.S, da + db};
+}
+// N further logits of a thread
+template <int N, bool WITH_D>
+__device__ __forceinline__ void accumulate(RowStat &s, const float (&l)[N], float c, double invT) {
+    float cm = l[0];
+#pragma unroll
+    for (int i = 1; i < N; i++) cm = fmaxf(cm, l[i]);
+    if (cm > s.m) {
+        if (s.m != -INFINITY) {
+            const double t = ((double)s.m - cm) * invT, e = exp_f64(t);
+            if (WITH_D) s.D = e * fma(t / LN2, s.S, s.D);
+            s.S *= e;
+        }
+        s.m = cm;
+    }
+    const float m = s.m == -INFINITY ? 0.0f : s.m;
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        const float x = (l[i] - m) * c, e = __builtin_amdgcn_exp2f(x);
+        s.S += (double)e;
+        if (WITH_D) s.D = fma((double)e, (double)fmaxf(x, -1e30f), s.D);      // (a token ruled out: 0 times a number)
+    }
+}
+__device__ __forceinline__ RowStat shfl_xor(const RowStat &s, int off) {
+    return RowStat{__shfl_xor(s.m, off), __shfl_xor(s.S, off), __shfl_xor(s.D, off)};
+}
+// over the workgroup, in a fixed order; every thread gets it
+template <int NW>
+__device__ __forceinline__ RowStat block_merge(RowStat s, double invT, RowStat *sm) {
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const RowStat o = shfl_xor(s, off);
+        s = (threadIdx.x & off) ? merge(o, s, invT) : merge(s, o, invT);
+    }
+    if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = s;
+    __syncthreads();
+    RowStat r = sm[0];
+#pragma unroll
+    for (int w = 1; w < NW; w++) r = merge(r, sm[w], invT);
+    __syncthreads();
+    return r;
+}
+
+constexpr int ROW_NT = 1024, ROW_NW = ROW_NT / 64;
+constexpr int ROW_PER = 16;                         // logits of a thread per step
+constexpr int WAVE_STEP = 64 * ROW_PER, ROW_STEP = ROW_NW * WAVE_STEP;
+typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));     // rows of an odd vocabulary begin anywhere
+
+// logit 4 q + e of a thread's step is column first + 256 q + e, first = the wave's first column + 4 lane; what lies behind the row is -infinity
+__device__ __forceinline__ void load_logits(const float *__restrict__ row, int first, int end, float (&l)[ROW_PER]) {
+#pragma unroll
+    for (int q = 0; q < ROW_PER / 4; q++) {
+        const int v = first + 256 * q;
+        if (v + 3 < end) {
+            const v4f f = *(const v4f_any *)(row + v);
+#pragma unroll
+            for (int e = 0; e < 4; e++) l[4 * q + e] = f[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; e++) l[4 * q + e] = v + e < end ? row[v + e] : -INFINITY;
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------ the largest logits of a row
+//
+// A wave keeps the 64 best keys it has seen, one per lane in falling order: (value, lower index first) as one 64-bit number.
+// A step's logits are compared with the last key that still counts, and what passes is inserted one by one; after the first
+// few hundred logits of random order that is rare.
+__device__ __forceinline__ uint32_t order_key(float f) {                   // orders like the floats (-0 as +0)
+    const uint32_t u = __float_as_uint(f + 0.0f);
+    return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+__device__ __forceinline__ float key_value(uint64_t key) {
+    const uint32_t u = (uint32_t)(key >> 32);
+    return __uint_as_float((u & 0x80000000u) ? u & 0x7fffffffu : ~u);
+}
+__device__ __forceinline__ int key_index(uint64_t key) { return (int)~(uint32_t)key; }
+__device__ __forceinline__ uint64_t read_lane(uint64_t v, int lane) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
+}
+struct TopList {
+    uint64_t key = 0, last = 0;         // this lane's key; the one at place top_k - 1
+    __device__ __forceinline__ void offer(uint64_t k, int top_k) {        // one key per lane, 0: none
+        const int lane = threadIdx.x & 63;
+        unsigned long long who = __ballot(k > last);
+        while (who) {
+            const int from = __builtin_ctzll(who);
+            const uint64_t nk = read_lane(k, from);
+            if (lane == from) k = 0;
+            const uint64_t prev = (uint64_t)dpp_move<0x138, 0xf>(0u, (uint32_t)(key >> 32)) << 32 | dpp_move<0x138, 0xf>(0u, (uint32_t)key);   // wave_shr 1
+            if (key < nk) key = lane == 0 || prev > nk ? nk : prev;
+            last = read_lane(key, top_k - 1);
+            who = __ballot(k > last);
+        }
+    }
+};
+
+__global__ void __launch_bounds__(ROW_NT) k_logprobs(const float *__restrict__ logits, const int32_t *__restrict__ tokens, int V,
+                                                     float temperature, int top_k, float *__restrict__ logprob,
+                                                     float *__restrict__ entropy, int32_t *__restrict__ top,
+                                                     float *__restrict__ top_logprob) {
+    __shared__ RowStat sm[ROW_NW];
+    __shared__ uint64_t lists[ROW_NW][64];
+    const int t = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const float *row = logits + (size_t)t * V;
+    const double invT = 1.0 / (double)temperature;
+    const float c = (float)(invT / LN2);
+    RowStat s{-INFINITY, 0.0, 0.0};
+    TopList list;
+    for (int v0 = wave * WAVE_STEP; v0 < V; v0 += ROW_STEP) {
+        float l[ROW_PER];
+        load_logits(row, v0 + 4 * lane, V, l);
+        accumulate<ROW_PER, true>(s, l, c, invT);
+        if (top_k) {
+#pragma unroll
+            for (int i = 0; i < ROW_PER; i++) {
+                const int v = v0 + 4 * lane + 256 * (i >> 2) + (i & 3);
+                list.offer(v < V ? (uint64_t)order_key(l[i]) << 32 | (uint32_t)~v : 0, top_k);
+            }
+        }
+    }
+    s = block_merge<ROW_NW>(s, invT, sm);
+    const double lse = log(s.S);                            // above (m / T)
+    const bool none = s.S == 0.0;
+    if (threadIdx.x == 0) {
+        if (logprob) {
+            const int v = tokens[t];
+            logprob[t] = v < 0 || v >= V ? 0.0f : none ? -INFINITY : (float)(((double)row[v] - s.m) * invT - lse);
+        }
+        if (entropy) entropy[t] = none ? 0.0f : (float)(lse - LN2 * s.D / s.S);
+    }
+    if (!top_k) return;
+    lists[wave][lane] = list.key;
+    __syncthreads();
+    if (wave) return;
+    for (int w = 1; w < ROW_NW; w++) list.offer(lists[w][lane], top_k);
+    if (lane < top_k) {
+        top[(size_t)t * top_k + lane] = key_index(list.key);
+        top_logprob[(size_t)t * top_k + lane] = none ? -INFINITY : (float)(((double)key_value(list.key) - s.m) * invT - lse);
+    }
+}
+
+// ------------------------------------------------------------------------------------ distillation
+//
+// Two passes of one workgroup over its row: the softmax statistics, then scale * q.  The list's columns get their gradient,
+// scale * (q - p) in fp64, after that.
+__global__ void __launch_bounds__(ROW_NT) k_distill(const float *logits, int V, const int32_t *__restrict__ ids,
+                                                    const float *__restrict__ vals, int K, float temperature,
+                                                    const float *__restrict__ loss_grad, float *__restrict__ loss, float *grad) {
+    __shared__ RowStat sm[ROW_NW];
+    __shared__ double sd[ROW_NW];
+    __shared__ float sf[ROW_NW];
+    __shared__ int s_id[PETALS_DISTILL_TOP_MAX];
+    __shared__ double s_p[PETALS_DISTILL_TOP_MAX];
+    static_assert(ROW_NT >= PETALS_DISTILL_TOP_MAX, "one entry of the list per thread");
+    const int t = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k = threadIdx.x;
+    const float *row = logits + (size_t)t * V;
+    float *out = grad + (size_t)t * V;
+    const double invT = 1.0 / (double)temperature;
+    const float c = (float)(invT / LN2);
+    // the teacher's distribution, one entry per thread
+    int id = -1;
+    float val = -INFINITY;
+    if (k < K) {
+        id = ids[(size_t)t * K + k];
+        if (id < 0 || id >= V) id = -1;
+        else val = vals[(size_t)t * K + k];
+    }
+    const float tm = block_max<ROW_NW>(val, sf);
+    const double tt = ((double)val - tm) * invT, te = id < 0 || val == -INFINITY ? 0.0 : exp_f64(tt);
+    const double tS = block_sum<ROW_NW>(te, sd), p = te / tS;
+    const bool listed = !(tS == 0.0);                                // (or NaN)
+    if (k < K) {
+        s_id[k] = id;
+        s_p[k] = p;
+    }
+    RowStat s{-INFINITY, 0.0, 0.0};
+    float l[ROW_PER];
+    if (listed) {
+        for (int v0 = wave * WAVE_STEP; v0 < V; v0 += ROW_STEP) {
+            load_logits(row, v0 + 4 * lane, V, l);
+            accumulate<ROW_PER, false>(s, l, c, invT);
+        }
+    }
+    s = block_merge<ROW_NW>(s, invT, sm);
+    const bool none = s.S == 0.0;
+    const double lse = log(s.S), w = listed && !none ? (double)temperature * (loss_grad ? (double)loss_grad[t] : 1.0) : 0.0;
+    // the list's own terms
+    double term = 0.0, at = 0.0;
+    if (id >= 0 && listed) {
+        const double z = ((double)row[id] - s.m) * invT;             // log q + lse
+        if (te > 0.0 || te != te) term = p * (tt - log(tS) - (z - lse));
+        double sum_p = 0.0;
+        for (int j = 0; j < K; j++)
+            if (s_id[j] == id) sum_p += s_p[j];
+        at = none ? 0.0 : w * (exp_f64(z) / s.S - sum_p);
+    }
+    const double total = block_sum<ROW_NW>(term, sd);
+    if (threadIdx.x == 0 && loss)
+        loss[t] = !listed ? 0.0f : none ? INFINITY : (float)((double)temperature * (double)temperature * total);
+    if (!grad) return;
+    const float f = (float)(none || !listed ? 0.0 : w / s.S), m = none || !listed ? 0.0f : s.m;
+    for (int v0 = wave * WAVE_STEP; v0 < V; v0 += ROW_STEP) {
+        if (!(none || !listed)) load_logits(row, v0 + 4 * lane, V, l);
+#pragma unroll
+        for (int q = 0; q < ROW_PER / 4; q++) {
+            const int v = v0 + 4 * lane + 256 * q;
+            v4f g;
+#pragma unroll
+            for (int e = 0; e < 4; e++) g[e] = none || !listed ? 0.0f : f * __builtin_amdgcn_exp2f((l[4 * q + e] - m) * c);
+            if (v + 3 < V) {
+                *(v4f_any *)(out + v) = g;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    if (v + e < V) out[v + e] = g[e];
+            }
+        }
+    }
+    __syncthreads();                                                 // the list's columns after the row
+    if (id >= 0 && listed && !none) out[id] = (float)at;             // (entries with the same token write the same)
+}
+
+// ------------------------------------------------------------------------------------ gradient of the lookup
+//
+// The LayerNorm's derivative is linear in the gradient, and its statistics belong to the token, not to the position: the
+// gradients of a token's positions are summed first and go through it once.
+//
+// Places in token order by counting: place of position i = number of j with (token_j, j) < (token_i, i).  No order of
+// atomics enters, and a call of a few thousand positions is a few million comparisons.
+struct Place {
+    int position, before, count;      // the position; how many earlier ones have its token, and how many in all
+};
+constexpr int RUN_PIECE = 32;         // positions that one workgroup sums; a longer list goes in pieces of 32 to 63
+
+__global__ void __launch_bounds__(1024) k_token_places(const int32_t *__restrict__ ids, int M, int V, Place *__restrict__ places) {
+    __shared__ int tile[1024];
+    __shared__ int less[16][64], same[16][64], all[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = blockIdx.x * 64 + lane;
+    const int own = i < M ? min(max(ids[i], 0), V - 1) : 0;
+    int n_less = 0, n_before = 0, n_all = 0;
+    for (int j0 = 0; j0 < M; j0 += 1024) {
+        const int j = j0 + threadIdx.x;
+        __syncthreads();
+        tile[threadIdx.x] = j < M ? min(max(ids[j], 0), V - 1) : 0x7fffffff;
+        __syncthreads();
+        for (int u = wave * 64; u < wave * 64 + 64; u++) {
+            const int o = tile[u];
+            n_less += o < own;
+            n_all += o == own;
+            n_before += o == own && j0 + u < i;
+        }
+    }
+    less[wave][lane] = n_less;
+    same[wave][lane] = n_before;
+    all[wave][lane] = n_all;
+    __syncthreads();
+    if (wave == 0 && i < M) {
+        n_less = n_before = n_all = 0;
+        for (int w = 0; w < 16; w++) {
+            n_less += less[w][lane];
+            n_before += same[w][lane];
+            n_all += all[w][lane];
+        }
+        places[n_less + n_before] = Place{i, n_before, n_all};
+    }
+}
+
+// How many pieces a list of n positions has, each of RUN_PIECE but the last, which takes what is left over as well
+__device__ __forceinline__ int run_pieces(int n) { return max(1, n / RUN_PIECE); }
+
+// number of different tokens before place p (over the workgroup)
+template <int NT>
+__device__ __forceinline__ int tokens_before(const Place *__restrict__ places, int p, int *sm) {
+    int n = 0;
+    for (int q = threadIdx.x; q < p; q += NT) n += places[q].before == 0;
+    n = (int)wave_sum((float)n);                                     // at most 2^24 of them
+    if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = n;
+    __syncthreads();
+    n = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 64; w++) n += sm[w];
+    __syncthreads();
+    return n;
+}
+
+// one workgroup per place: a place at which a piece of a token's list begins has work
+template <int NT, int PER>
+__global__ void __launch_bounds__(NT) k_embed_backward(const int32_t *__restrict__ ids, const __half *__restrict__ grad, int M, int V,
+                                                       int H, const __half *__restrict__ E, const __half *__restrict__ g, float eps,
+                                                       const Place *__restrict__ places, float *__restrict__ parts,
+                                                       int32_t *__restrict__ tokens_out, float *__restrict__ grads_out,
+                                                       int32_t *__restrict__ count_out) {
+    __shared__ double sd[NT / 64][2];
+    __shared__ int si[NT / 64];
+    const int p = blockIdx.x;
+    const Place pl = places[p];
+    const int piece = pl.before / RUN_PIECE, pieces = run_pieces(pl.count);
+    if (pl.before % RUN_PIECE || piece >= pieces) {
+        if (p == M - 1) {                                            // not the first of its token: the count is still to be told
+            const int n = tokens_before<NT>(places, M, si);
+            if (threadIdx.x == 0) *count_out = n;
+        }
+        return;
+    }
+    const int n = piece == pieces - 1 ? pl.count - pl.before : RUN_PIECE;
+    float acc[PER][8];
+#pragma unroll
+    for (int i = 0; i < PER; i++)
+#pragma unroll
+        for (int e = 0; e < 8; e++) acc[i][e] = 0.0f;
+    for (int r = 0; r < n; r++) {
+        const __half *row = grad + (size_t)places[p + r].position * H;
+#pragma unroll
+        for (int i = 0; i < PER; i++) {
+            const int k = (threadIdx.x + i * NT) * 8;
+            if (k < H) {
+                const v8h f = *(const v8h_any *)(row + k);
+#pragma unroll
+                for (int e = 0; e < 8; e++) acc[i][e] += (float)f[e];
+            }
+        }
+    }
+    if (pieces > 1) {                                                // pieces begin at least RUN_PIECE places apart
+        ln_store<NT, PER>(acc, parts + (size_t)(p / RUN_PIECE) * H, H);
+    } else {
+        const int u = tokens_before<NT>(places, p, si), token = min(max(ids[pl.position], 0), V - 1);
+        ln_backward<NT, PER>(acc, E + (size_t)token * H, g, H, eps, sd);
+        ln_store<NT, PER>(acc, grads_out + (size_t)u * H, H);
+        if (threadIdx.x == 0) tokens_out[u] = token;
+    }
+    if (p == M - 1) {
+        const int all = tokens_before<NT>(places, M, si);
+        if (threadIdx.x == 0) *count_out = all;
+    }
+}
+
+// the lists of several pieces: workgroup b looks for one that begins at places b * RUN_PIECE ..
+template <int NT, int PER>
+__global__ void __launch_bounds__(NT) k_embed_backward_join(const int32_t *__restrict__ ids, int M, int V, int H,
+                                                            const __half *__restrict__ E, const __half *__restrict__ g, float eps,
+                                                            const Place *__restrict__ places, const float *__restrict__ parts,
+                                                            int32_t *__restrict__ tokens_out, float *__restrict__ grads_out) {
+    __shared__ double sd[NT / 64][2];
+    __shared__ int si[NT / 64];
+    __shared__ int s_at;
+    if (threadIdx.x == 0) s_at = -1;
+    __syncthreads();
+    const int q = blockIdx.x * RUN_PIECE + threadIdx.x;
+    if (threadIdx.x < RUN_PIECE && q < M && places[q].before == 0 && run_pieces(places[q].count) > 1) s_at = q;      // at most one
+    __syncthreads();
+    const int p = s_at;
+    if (p < 0) return;
+    const Place pl = places[p];
+    const int pieces = run_pieces(pl.count), token = min(max(ids[pl.position], 0), V - 1);
+    float acc[PER][8];
+#pragma unroll
+    for (int i = 0; i < PER; i++)
+#pragma unroll
+        for (int e = 0; e < 8; e++) acc[i][e] = 0.0f;
+    for (int r = 0; r < pieces; r++) {
+        const float *row = parts + (size_t)((p + r * RUN_PIECE) / RUN_PIECE) * H;
+#pragma unroll
+        for (int i = 0; i < PER; i++) {
+            const int k = (threadIdx.x + i * NT) * 8;
+            if (k < H) {
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    const v4f f = *(const v4f *)(row + k + 4 * h);
+#pragma unroll
+                    for (int e = 0; e < 4; e++) acc[i][4 * h + e] += f[e];
+                }
+            }
+        }
+    }
+    const int u = tokens_before<NT>(places, p, si);
+    ln_backward<NT, PER>(acc, E + (size_t)token * H, g, H, eps, sd);
+    ln_store<NT, PER>(acc, grads_out + (size_t)u * H, H);
+    if (threadIdx.x == 0) tokens_out[u] = token;
+}
+
+template <int NT, int PER>
+void embed_backward(const int32_t *ids, const __half *grad, int M, int V, int H, const __half *E, const __half *g, float eps,
+                    const Place *places, float *parts, int32_t *tokens_out, float *grads_out, int32_t *count_out, hipStream_t st) {
+    k_embed_backward<NT, PER><<<M, NT, 0, st>>>(ids, grad, M, V, H, E, g, eps, places, parts, tokens_out, grads_out, count_out);
+    if (M >= 2 * RUN_PIECE)
+        k_embed_backward_join<NT, PER><<<(M + RUN_PIECE - 1) / RUN_PIECE, NT, 0, st>>>(ids, M, V, H, E, g, eps, places, parts, tokens_out, grads_out);
+}
+
+int check_call(const petals_client_config &cfg, int32_t M) {
+    if (M < 1) return ps_fail(PETALS_ERR_INVALID_ARG, "M must be positive");
+    if (M > cfg.max_rows_per_call) return ps_fail(PETALS_ERR_CAPACITY, "%d rows exceed max_rows_per_call %d", M, cfg.max_rows_per_call);
+    return PETALS_OK;
+}
+bool usable_temperature(float t) { return t > 0.0f && t < INFINITY && 1.0f / t < INFINITY; }
+
+}  // namespace
+
+extern "C" {
+
+int petals_client_logprobs(petals_client *client, const float *logits, const int32_t *tokens, int32_t M, float temperature,
+                           int32_t top_k, float *logprob_out, float *entropy_out, int32_t *top_out, float *top_logprob_out,
+                           void *stream) {
+    if (!client || !logits) return ps_fail(PETALS_ERR_INVALID_ARG, "null pointer");
+    const ps_client_view c = ps_view(client);
+    if (int rc = check_call(*c.cfg, M)) return rc;
+    if (!tokens != !logprob_out) return ps_fail(PETALS_ERR_INVALID_ARG, "tokens and logprob_out go together");
+    if (top_k < 0) return ps_fail(PETALS_ERR_INVALID_ARG, "top_k must not be negative");
+    if (top_k > PETALS_LOGPROBS_TOP_MAX) return ps_fail(PETALS_ERR_UNSUPPORTED, "top_k %d exceeds %d", top_k, PETALS_LOGPROBS_TOP_MAX);
+    if (top_k > c.cfg->vocab) return ps_fail(PETALS_ERR_INVALID_ARG, "top_k %d exceeds the vocabulary %d", top_k, c.cfg->vocab);
+    if ((top_k > 0) != (top_out != nullptr) || (top_k > 0) != (top_logprob_out != nullptr))
+        return ps_fail(PETALS_ERR_INVALID_ARG, "top_out and top_logprob_out go with top_k > 0");
+    if (!logprob_out && !entropy_out && !top_out) return ps_fail(PETALS_ERR_INVALID_ARG, "no output requested");
+    if (!usable_temperature(temperature)) return ps_fail(PETALS_ERR_INVALID_ARG, "temperature must be positive and finite");
+    k_logprobs<<<M, ROW_NT, 0, (hipStream_t)stream>>>(logits, tokens, c.cfg->vocab, temperature, top_k, logprob_out, entropy_out, top_out, top_logprob_out);
+    HIP_TRY(hipGetLastError());
+    return PETALS_OK;
+}
+
+int petals_client_distill(petals_client *client, const float *logits, int32_t M, const int32_t *teacher_tokens,
+                          const float *teacher_logits, int32_t K, float temperature, const float *loss_grad, float *loss_out,
+                          float *grad_logits_out, void *stream) {
+    if (!client || !logits || !teacher_tokens || !teacher_logits) return ps_fail(PETALS_ERR_INVALID_ARG, "null pointer");
+    const ps_client_view c = ps_view(client);
+    if (int rc = check_call(*c.cfg, M)) return rc;
+    if (K < 1) return ps_fail(PETALS_ERR_INVALID_ARG, "K must be positive");
+    if (K > PETALS_DISTILL_TOP_MAX) return ps_fail(PETALS_ERR_UNSUPPORTED, "K %d exceeds %d", K, PETALS_DISTILL_TOP_MAX);
+    if (!loss_out && !grad_logits_out) return ps_fail(PETALS_ERR_INVALID_ARG, "neither loss nor gradient requested");
+    if (!usable_temperature(temperature)) return ps_fail(PETALS_ERR_INVALID_ARG, "temperature must be positive and finite");
+    k_distill<<<M, ROW_NT, 0, (hipStream_t)stream>>>(logits, c.cfg->vocab, teacher_tokens, teacher_logits, K, temperature, loss_grad, loss_out,
+                                                     grad_logits_out);
+    HIP_TRY(hipGetLastError());
+    return PETALS_OK;
+}
+
+int petals_client_embed_backward(petals_client *client, const int32_t *token_ids, const void *grad_hidden, int32_t M,
+                                 int32_t *tokens_out, float *grads_out, int32_t *count_out, void *stream) {
+    if (!client || !token_ids || !grad_hidden || !tokens_out || !grads_out || !count_out) return ps_fail(PETALS_ERR_INVALID_ARG, "null pointer");
+    const ps_client_view c = ps_view(client);
+    if (int rc = check_call(*c.cfg, M)) return rc;
+    if (token_ids == tokens_out) return ps_fail(PETALS_ERR_INVALID_ARG, "token_ids and tokens_out alias");
+    const int V = c.cfg->vocab, H = c.cfg->hidden;
+    // M places of 12 bytes, then a row of partial sums for every RUN_PIECE places: 12 M + (M / 32 + 1) 4 H bytes
+    Place *places = (Place *)c.scratch;
+    float *parts = (float *)(c.scratch + ((size_t)M * sizeof(Place) + 255) / 256 * 256);
+    hipStream_t st = (hipStream_t)stream;
+    const __half *E = (const __half *)c.p->embeddings, *g = (const __half *)c.p->emb_ln_g, *gr = (const __half *)grad_hidden;
+    const float eps = c.cfg->ln_eps;
+    k_token_places<<<(M + 63) / 64, 1024, 0, st>>>(token_ids, M, V, places);
+    if (H <= 2048) embed_backward<256, 1>(token_ids, gr, M, V, H, E, g, eps, places, parts, tokens_out, grads_out, count_out, st);
+    else if (H <= 4096) embed_backward<512, 1>(token_ids, gr, M, V, H, E, g, eps, places, parts, tokens_out, grads_out, count_out, st);
+    else if (H <= 8192) embed_backward<1024, 1>(token_ids, gr, M, V, H, E, g, eps, places, parts, tokens_out, grads_out, count_out, st);
+    else embed_backward<1024, 2>(token_ids, gr, M, V, H, E, g, eps, places, parts, tokens_out, grads_out, count_out, st);
+    HIP_TRY(hipGetLastError());
+    return PETALS_OK;
+}
+
+}  // extern "C"
