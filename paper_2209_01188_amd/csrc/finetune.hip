@@ -31,9 +31,9 @@ __device__ __forceinline__ RowStat merge(const RowStat &a, const RowStat &b, dou
     const double da = a.m == -INFINITY ? 0.0 : ea * fma(ta / LN2, a.S, a.D), db = b.m == -INFINITY ? 0.0 : eb * fma(tb / LN2, b.S, b.D);
     return RowStat{m, ea * a.S + eb * b.S, da + db};
 }
-// N further logits of a thread
+// N further logits of a thread; returns the largest of them
 template <int N, bool WITH_D>
-__device__ __forceinline__ void accumulate(RowStat &s, const float (&l)[N], float c, double invT) {
+__device__ __forceinline__ float accumulate(RowStat &s, const float (&l)[N], float c, double invT) {
     float cm = l[0];
 #pragma unroll
     for (int i = 1; i < N; i++) cm = fmaxf(cm, l[i]);
@@ -50,8 +50,9 @@ __device__ __forceinline__ void accumulate(RowStat &s, const float (&l)[N], floa
     for (int i = 0; i < N; i++) {
         const float x = (l[i] - m) * c, e = __builtin_amdgcn_exp2f(x);
         s.S += (double)e;
-        if (WITH_D) s.D = fma((double)e, (double)fmaxf(x, -1e30f), s.D);      // (a token ruled out: 0 times a number)
+        if (WITH_D) s.D += (double)(e * fmaxf(x, -1e30f));                    // (a token ruled out: 0 times a number)
     }
+    return cm;
 }
 __device__ __forceinline__ RowStat shfl_xor(const RowStat &s, int off) {
     return RowStat{__shfl_xor(s.m, off), __shfl_xor(s.S, off), __shfl_xor(s.D, off)};
@@ -73,10 +74,20 @@ __device__ __forceinline__ RowStat block_merge(RowStat s, double invT, RowStat *
     return r;
 }
 
-constexpr int ROW_NT = 1024, ROW_NW = ROW_NT / 64;
+constexpr int ROW_NT = 256, ROW_NW = ROW_NT / 64;
 constexpr int ROW_PER = 16;                         // logits of a thread per step
 constexpr int WAVE_STEP = 64 * ROW_PER, ROW_STEP = ROW_NW * WAVE_STEP;
+constexpr int ROW_GROUPS = 2048;                    // workgroups that fill the chip: 8 per compute unit
 typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));     // rows of an odd vocabulary begin anywhere
+
+// A call of few rows shares each row out over workgroups, a whole number of steps to each.
+struct RowSplit {
+    int splits, range;
+};
+RowSplit row_split(int M, int V, int most) {
+    const int steps = (V + ROW_STEP - 1) / ROW_STEP, want = max(1, min(most, (ROW_GROUPS + M - 1) / M)), per = (steps + min(steps, want) - 1) / min(steps, want);
+    return RowSplit{(steps + per - 1) / per, per * ROW_STEP};
+}
 
 // logit 4 q + e of a thread's step is column first + 256 q + e, first = the wave's first column + 4 lane; what lies behind the row is -infinity
 __device__ __forceinline__ void load_logits(const float *__restrict__ row, int first, int end, float (&l)[ROW_PER]) {
@@ -113,6 +124,10 @@ __device__ __forceinline__ uint64_t read_lane(uint64_t v, int lane) {
 }
 struct TopList {
     uint64_t key = 0, last = 0;         // this lane's key; the one at place top_k - 1
+    __device__ __forceinline__ void start(uint64_t k, int top_k) {        // a list that is in order already
+        key = k;
+        last = read_lane(key, top_k - 1);
+    }
     __device__ __forceinline__ void offer(uint64_t k, int top_k) {        // one key per lane, 0: none
         const int lane = threadIdx.x & 63;
         unsigned long long who = __ballot(k > last);
@@ -128,130 +143,282 @@ struct TopList {
     }
 };
 
-__global__ void __launch_bounds__(ROW_NT) k_logprobs(const float *__restrict__ logits, const int32_t *__restrict__ tokens, int V,
-                                                     float temperature, int top_k, float *__restrict__ logprob,
-                                                     float *__restrict__ entropy, int32_t *__restrict__ top,
-                                                     float *__restrict__ top_logprob) {
-    __shared__ RowStat sm[ROW_NW];
-    __shared__ uint64_t lists[ROW_NW][64];
-    const int t = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const float *row = logits + (size_t)t * V;
-    const double invT = 1.0 / (double)temperature;
-    const float c = (float)(invT / LN2);
-    RowStat s{-INFINITY, 0.0, 0.0};
-    TopList list;
-    for (int v0 = wave * WAVE_STEP; v0 < V; v0 += ROW_STEP) {
-        float l[ROW_PER];
-        load_logits(row, v0 + 4 * lane, V, l);
-        accumulate<ROW_PER, true>(s, l, c, invT);
-        if (top_k) {
-#pragma unroll
-            for (int i = 0; i < ROW_PER; i++) {
-                const int v = v0 + 4 * lane + 256 * (i >> 2) + (i & 3);
-                list.offer(v < V ? (uint64_t)order_key(l[i]) << 32 | (uint32_t)~v : 0, top_k);
-            }
-        }
-    }
-    s = block_merge<ROW_NW>(s, invT, sm);
+struct LogprobsOut {
+    const float *logits;
+    const int32_t *tokens;
+    float *logprob, *entropy;
+    int32_t *top;
+    float *top_logprob;
+};
+// the results of a row from its statistics (in every thread) and, in the first wave, its list
+__device__ __forceinline__ void logprobs_store(const LogprobsOut &o, int t, int V, double invT, int top_k, const RowStat &s, const TopList &list) {
     const double lse = log(s.S);                            // above (m / T)
     const bool none = s.S == 0.0;
     if (threadIdx.x == 0) {
-        if (logprob) {
-            const int v = tokens[t];
-            logprob[t] = v < 0 || v >= V ? 0.0f : none ? -INFINITY : (float)(((double)row[v] - s.m) * invT - lse);
+        if (o.logprob) {
+            const int v = o.tokens[t];
+            o.logprob[t] = v < 0 || v >= V ? 0.0f : none ? -INFINITY : (float)(((double)o.logits[(size_t)t * V + v] - s.m) * invT - lse);
         }
-        if (entropy) entropy[t] = none ? 0.0f : (float)(lse - LN2 * s.D / s.S);
+        if (o.entropy) o.entropy[t] = none ? 0.0f : (float)(lse - LN2 * s.D / s.S);
     }
-    if (!top_k) return;
+    if ((int)threadIdx.x < top_k) {                         // at most 64
+        o.top[(size_t)t * top_k + threadIdx.x] = key_index(list.key);
+        o.top_logprob[(size_t)t * top_k + threadIdx.x] = none ? -INFINITY : (float)(((double)key_value(list.key) - s.m) * invT - lse);
+    }
+}
+// the waves' lists become the first wave's
+__device__ __forceinline__ void join_lists(TopList &list, uint64_t (*lists)[64], int top_k) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     lists[wave][lane] = list.key;
     __syncthreads();
-    if (wave) return;
-    for (int w = 1; w < ROW_NW; w++) list.offer(lists[w][lane], top_k);
-    if (lane < top_k) {
-        top[(size_t)t * top_k + lane] = key_index(list.key);
-        top_logprob[(size_t)t * top_k + lane] = none ? -INFINITY : (float)(((double)key_value(list.key) - s.m) * invT - lse);
+    if (wave == 0)
+        for (int w = 1; w < ROW_NW; w++) list.offer(lists[w][lane], top_k);
+}
+
+// workgroup (split, row): the split's part of the row, and with one split the results
+__global__ void __launch_bounds__(ROW_NT) k_logprobs(LogprobsOut o, int V, int range, double invT, int top_k, RowStat *__restrict__ stats,
+                                                     uint64_t *__restrict__ tops) {
+    __shared__ RowStat sm[ROW_NW];
+    __shared__ uint64_t lists[ROW_NW][64];
+    const int t = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const float *row = o.logits + (size_t)t * V;
+    const float c = (float)(invT / LN2);
+    const int end = min(V, ((int)blockIdx.x + 1) * range);
+    RowStat s{-INFINITY, 0.0, 0.0};
+    TopList list;
+    int v0 = blockIdx.x * range + wave * WAVE_STEP;
+    float l[ROW_PER], ahead[ROW_PER];
+    if (v0 < end) load_logits(row, v0 + 4 * lane, end, l);
+    for (; v0 < end; v0 += ROW_STEP) {
+        if (v0 + ROW_STEP < end) load_logits(row, v0 + ROW_STEP + 4 * lane, end, ahead);
+        const float most = accumulate<ROW_PER, true>(s, l, c, invT);
+        if (top_k && __ballot(!(most < key_value(list.last)))) {
+#pragma unroll
+            for (int i = 0; i < ROW_PER; i++) {
+                const int v = v0 + 4 * lane + 256 * (i >> 2) + (i & 3);
+                list.offer(v < end ? (uint64_t)order_key(l[i]) << 32 | (uint32_t)~v : 0, top_k);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < ROW_PER; i++) l[i] = ahead[i];
     }
+    s = block_merge<ROW_NW>(s, invT, sm);
+    if (top_k) join_lists(list, lists, top_k);
+    if (gridDim.x == 1) {
+        logprobs_store(o, t, V, invT, top_k, s, list);
+        return;
+    }
+    const size_t at = (size_t)t * gridDim.x + blockIdx.x;
+    if (threadIdx.x == 0) stats[at] = s;
+    if ((int)threadIdx.x < top_k) tops[at * top_k + threadIdx.x] = list.key;
+}
+
+// what the splits of a row have found
+__global__ void __launch_bounds__(ROW_NT) k_logprobs_join(LogprobsOut o, int V, int splits, double invT, int top_k,
+                                                          const RowStat *__restrict__ stats, const uint64_t *__restrict__ tops) {
+    __shared__ RowStat sm[ROW_NW];
+    __shared__ uint64_t lists[ROW_NW][64];
+    const int t = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    RowStat s{-INFINITY, 0.0, 0.0};
+    for (int i = threadIdx.x; i < splits; i += ROW_NT) s = merge(s, stats[(size_t)t * splits + i], invT);
+    s = block_merge<ROW_NW>(s, invT, sm);
+    TopList list;
+    if (top_k) {
+        for (int i = wave; i < splits; i += ROW_NW) {
+            const uint64_t k = lane < top_k ? tops[((size_t)t * splits + i) * top_k + lane] : 0;
+            if (i == wave) list.start(k, top_k);
+            else list.offer(k, top_k);
+        }
+        join_lists(list, lists, top_k);
+    }
+    logprobs_store(o, t, V, invT, top_k, s, list);
 }
 
 // ------------------------------------------------------------------------------------ distillation
 //
-// Two passes of one workgroup over its row: the softmax statistics, then scale * q.  The list's columns get their gradient,
-// scale * (q - p) in fp64, after that.
-__global__ void __launch_bounds__(ROW_NT) k_distill(const float *logits, int V, const int32_t *__restrict__ ids,
-                                                    const float *__restrict__ vals, int K, float temperature,
-                                                    const float *__restrict__ loss_grad, float *__restrict__ loss, float *grad) {
+// Two passes over the logits, the softmax statistics and then w q, in launches of their own for calls of few rows, whose rows
+// are shared out over workgroups.  With x = z / T - max / T, log q = x - log S, so a part of the list (the entries whose
+// tokens lie in a workgroup's range) adds sum p (log p - z / T) and sum p to the loss, and the rest is the row's alone.
+struct DistillPart {
+    float m;
+    double S, term, mass;
+};
+struct DistillIn {
+    const float *logits;
+    const int32_t *ids;
+    const float *vals;
+    const float *loss_grad;
+    float *loss, *grad;
+    int V, K;
+    double T, invT;
+};
+constexpr int LIST_PER = (PETALS_DISTILL_TOP_MAX + ROW_NT - 1) / ROW_NT;
+struct Teacher {                       // entry k = i ROW_NT + threadIdx.x; id -1: none
+    int id[LIST_PER];
+    double p[LIST_PER], logp[LIST_PER];
+    bool listed;
+};
+template <int NT>
+__device__ __forceinline__ void teacher_row(const DistillIn &d, int t, Teacher &te, float *sf, double *sd) {
+    float val[LIST_PER], mx = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < LIST_PER; i++) {
+        const int k = i * NT + threadIdx.x;
+        te.id[i] = -1;
+        val[i] = -INFINITY;
+        if (k < d.K) {
+            const int id = d.ids[(size_t)t * d.K + k];
+            if (id >= 0 && id < d.V) {
+                te.id[i] = id;
+                val[i] = d.vals[(size_t)t * d.K + k];
+            }
+        }
+        mx = fmaxf(mx, val[i]);
+    }
+    mx = block_max<NT / 64>(mx, sf);
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < LIST_PER; i++) {
+        te.logp[i] = ((double)val[i] - mx) * d.invT;
+        te.p[i] = val[i] == -INFINITY ? 0.0 : exp_f64(te.logp[i]);
+        sum += te.p[i];
+    }
+    sum = block_sum<NT / 64>(sum, sd);
+    te.listed = !(sum == 0.0);                             // (or NaN)
+    const double ls = log(sum);
+#pragma unroll
+    for (int i = 0; i < LIST_PER; i++) {
+        te.p[i] /= sum;
+        te.logp[i] -= ls;
+    }
+}
+
+// workgroup (split, row)
+__global__ void __launch_bounds__(ROW_NT) k_distill_stats(DistillIn d, int range, DistillPart *__restrict__ parts) {
+    __shared__ RowStat sm[ROW_NW];
+    __shared__ double sd[ROW_NW];
+    __shared__ float sf[ROW_NW];
+    const int t = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const float *row = d.logits + (size_t)t * d.V;
+    const float c = (float)(d.invT / LN2);
+    const int begin = blockIdx.x * range, end = min(d.V, begin + range);
+    Teacher te;
+    teacher_row<ROW_NT>(d, t, te, sf, sd);
+    if (!te.listed) return;                                // nobody reads the part
+    double term = 0.0, mass = 0.0;
+#pragma unroll
+    for (int i = 0; i < LIST_PER; i++)
+        if (te.id[i] >= begin && te.id[i] < end && !(te.p[i] == 0.0)) {
+            term += te.p[i] * (te.logp[i] - (double)row[te.id[i]] * d.invT);
+            mass += te.p[i];
+        }
+    RowStat s{-INFINITY, 0.0, 0.0};
+    int v0 = begin + wave * WAVE_STEP;
+    float l[ROW_PER], ahead[ROW_PER];
+    if (v0 < end) load_logits(row, v0 + 4 * lane, end, l);
+    for (; v0 < end; v0 += ROW_STEP) {
+        if (v0 + ROW_STEP < end) load_logits(row, v0 + ROW_STEP + 4 * lane, end, ahead);
+        accumulate<ROW_PER, false>(s, l, c, d.invT);
+#pragma unroll
+        for (int i = 0; i < ROW_PER; i++) l[i] = ahead[i];
+    }
+    s = block_merge<ROW_NW>(s, d.invT, sm);
+    term = block_sum<ROW_NW>(term, sd);
+    mass = block_sum<ROW_NW>(mass, sd);
+    if (threadIdx.x == 0) parts[(size_t)t * gridDim.x + blockIdx.x] = DistillPart{s.m, s.S, term, mass};
+}
+
+// The gradient of a workgroup's range (logits and gradient may be the same memory: what a thread overwrites it has read, and
+// other threads' logits it reads before the barrier), and by the first workgroup of the row its loss.  The list's columns get
+// theirs, w (q - p) in fp64, after the others.
+__global__ void __launch_bounds__(ROW_NT) k_distill_grad(DistillIn d, int range, int splits, const DistillPart *__restrict__ parts) {
     __shared__ RowStat sm[ROW_NW];
     __shared__ double sd[ROW_NW];
     __shared__ float sf[ROW_NW];
     __shared__ int s_id[PETALS_DISTILL_TOP_MAX];
     __shared__ double s_p[PETALS_DISTILL_TOP_MAX];
-    static_assert(ROW_NT >= PETALS_DISTILL_TOP_MAX, "one entry of the list per thread");
-    const int t = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k = threadIdx.x;
-    const float *row = logits + (size_t)t * V;
-    float *out = grad + (size_t)t * V;
-    const double invT = 1.0 / (double)temperature;
-    const float c = (float)(invT / LN2);
-    // the teacher's distribution, one entry per thread
-    int id = -1;
-    float val = -INFINITY;
-    if (k < K) {
-        id = ids[(size_t)t * K + k];
-        if (id < 0 || id >= V) id = -1;
-        else val = vals[(size_t)t * K + k];
-    }
-    const float tm = block_max<ROW_NW>(val, sf);
-    const double tt = ((double)val - tm) * invT, te = id < 0 || val == -INFINITY ? 0.0 : exp_f64(tt);
-    const double tS = block_sum<ROW_NW>(te, sd), p = te / tS;
-    const bool listed = !(tS == 0.0);                                // (or NaN)
-    if (k < K) {
-        s_id[k] = id;
-        s_p[k] = p;
-    }
+    const int t = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const float *row = d.logits + (size_t)t * d.V;
+    const float c = (float)(d.invT / LN2);
+    const int begin = blockIdx.x * range, end = min(d.V, begin + range);
+    Teacher te;
+    teacher_row<ROW_NT>(d, t, te, sf, sd);
     RowStat s{-INFINITY, 0.0, 0.0};
-    float l[ROW_PER];
-    if (listed) {
-        for (int v0 = wave * WAVE_STEP; v0 < V; v0 += ROW_STEP) {
-            load_logits(row, v0 + 4 * lane, V, l);
-            accumulate<ROW_PER, false>(s, l, c, invT);
+    double term = 0.0, mass = 0.0;
+    if (te.listed) {
+        for (int i = threadIdx.x; i < splits; i += ROW_NT) {
+            const DistillPart p = parts[(size_t)t * splits + i];
+            s = merge(s, RowStat{p.m, p.S, 0.0}, d.invT);
+            term += p.term;
+            mass += p.mass;
         }
     }
-    s = block_merge<ROW_NW>(s, invT, sm);
+    s = block_merge<ROW_NW>(s, d.invT, sm);
     const bool none = s.S == 0.0;
-    const double lse = log(s.S), w = listed && !none ? (double)temperature * (loss_grad ? (double)loss_grad[t] : 1.0) : 0.0;
-    // the list's own terms
-    double term = 0.0, at = 0.0;
-    if (id >= 0 && listed) {
-        const double z = ((double)row[id] - s.m) * invT;             // log q + lse
-        if (te > 0.0 || te != te) term = p * (tt - log(tS) - (z - lse));
-        double sum_p = 0.0;
-        for (int j = 0; j < K; j++)
-            if (s_id[j] == id) sum_p += s_p[j];
-        at = none ? 0.0 : w * (exp_f64(z) / s.S - sum_p);
+    if (blockIdx.x == 0 && d.loss) {
+        term = block_sum<ROW_NW>(term, sd);
+        mass = block_sum<ROW_NW>(mass, sd);
+        if (threadIdx.x == 0)
+            d.loss[t] = !te.listed ? 0.0f : none ? INFINITY : (float)(d.T * d.T * (term + mass * ((double)s.m * d.invT + log(s.S))));
     }
-    const double total = block_sum<ROW_NW>(term, sd);
-    if (threadIdx.x == 0 && loss)
-        loss[t] = !listed ? 0.0f : none ? INFINITY : (float)((double)temperature * (double)temperature * total);
-    if (!grad) return;
-    const float f = (float)(none || !listed ? 0.0 : w / s.S), m = none || !listed ? 0.0f : s.m;
-    for (int v0 = wave * WAVE_STEP; v0 < V; v0 += ROW_STEP) {
-        if (!(none || !listed)) load_logits(row, v0 + 4 * lane, V, l);
+    if (!d.grad) return;
+    float *out = d.grad + (size_t)t * d.V;
+    const bool zero = !te.listed || none;
+    const double w = d.T * (d.loss_grad ? (double)d.loss_grad[t] : 1.0);
+    bool mine = false;
+#pragma unroll
+    for (int i = 0; i < LIST_PER; i++) {
+        const int k = i * ROW_NT + threadIdx.x;
+        if (k < d.K) {
+            s_id[k] = te.id[i];
+            s_p[k] = te.p[i];
+        }
+        if (zero || te.id[i] < begin || te.id[i] >= end) te.id[i] = -1;
+        mine |= te.id[i] >= 0;
+    }
+    __syncthreads();
+    float at[LIST_PER];
+    if (mine) {
+#pragma unroll
+        for (int i = 0; i < LIST_PER; i++) {
+            if (te.id[i] < 0) continue;
+            double p = 0.0;
+            for (int j = 0; j < d.K; j++) p += s_id[j] == te.id[i] ? s_p[j] : 0.0;
+            at[i] = (float)(w * (exp_f64(((double)row[te.id[i]] - s.m) * d.invT) / s.S - p));
+        }
+    }
+    __syncthreads();
+    const float f = zero ? 0.0f : (float)(w / s.S), m = zero ? 0.0f : s.m;
+    int v0 = begin + wave * WAVE_STEP;
+    float l[ROW_PER], ahead[ROW_PER];
+#pragma unroll
+    for (int i = 0; i < ROW_PER; i++) l[i] = ahead[i] = 0.0f;
+    if (v0 < end && !zero) load_logits(row, v0 + 4 * lane, end, l);
+    for (; v0 < end; v0 += ROW_STEP) {
+        if (v0 + ROW_STEP < end && !zero) load_logits(row, v0 + ROW_STEP + 4 * lane, end, ahead);
 #pragma unroll
         for (int q = 0; q < ROW_PER / 4; q++) {
             const int v = v0 + 4 * lane + 256 * q;
             v4f g;
 #pragma unroll
-            for (int e = 0; e < 4; e++) g[e] = none || !listed ? 0.0f : f * __builtin_amdgcn_exp2f((l[4 * q + e] - m) * c);
-            if (v + 3 < V) {
-                *(v4f_any *)(out + v) = g;
+            for (int e = 0; e < 4; e++) g[e] = zero ? 0.0f : f * __builtin_amdgcn_exp2f((l[4 * q + e] - m) * c);
+            if (v + 3 < end) {
+                __builtin_nontemporal_store(g, (v4f_any *)(out + v));
             } else {
 #pragma unroll
                 for (int e = 0; e < 4; e++)
-                    if (v + e < V) out[v + e] = g[e];
+                    if (v + e < end) out[v + e] = g[e];
             }
         }
+#pragma unroll
+        for (int i = 0; i < ROW_PER; i++) l[i] = ahead[i];
     }
-    __syncthreads();                                                 // the list's columns after the row
-    if (id >= 0 && listed && !none) out[id] = (float)at;             // (entries with the same token write the same)
+    __syncthreads();
+    if (mine) {
+#pragma unroll
+        for (int i = 0; i < LIST_PER; i++)
+            if (te.id[i] >= 0) out[te.id[i]] = at[i];      // (entries with the same token write the same)
+    }
 }
 
 // ------------------------------------------------------------------------------------ gradient of the lookup
@@ -425,6 +592,7 @@ int check_call(const petals_client_config &cfg, int32_t M) {
     if (M > cfg.max_rows_per_call) return ps_fail(PETALS_ERR_CAPACITY, "%d rows exceed max_rows_per_call %d", M, cfg.max_rows_per_call);
     return PETALS_OK;
 }
+constexpr int MAX_GRID_ROWS = 1 << 15;      // rows of one launch (the grid's second dimension)
 bool usable_temperature(float t) { return t > 0.0f && t < INFINITY && 1.0f / t < INFINITY; }
 
 }  // namespace
@@ -445,8 +613,26 @@ int petals_client_logprobs(petals_client *client, const float *logits, const int
         return ps_fail(PETALS_ERR_INVALID_ARG, "top_out and top_logprob_out go with top_k > 0");
     if (!logprob_out && !entropy_out && !top_out) return ps_fail(PETALS_ERR_INVALID_ARG, "no output requested");
     if (!usable_temperature(temperature)) return ps_fail(PETALS_ERR_INVALID_ARG, "temperature must be positive and finite");
-    k_logprobs<<<M, ROW_NT, 0, (hipStream_t)stream>>>(logits, tokens, c.cfg->vocab, temperature, top_k, logprob_out, entropy_out, top_out, top_logprob_out);
-    HIP_TRY(hipGetLastError());
+    hipStream_t st = (hipStream_t)stream;
+    const int V = c.cfg->vocab;
+    const double invT = 1.0 / (double)temperature;
+    // per row and split in the workspace: its statistics and its list
+    const size_t per = sizeof(RowStat) + sizeof(uint64_t) * top_k;
+    const RowSplit sp = row_split(M, V, (int)min((size_t)1 << 20, c.scratch_bytes / ((size_t)M * per)));
+    RowStat *stats = (RowStat *)c.scratch;
+    uint64_t *tops = (uint64_t *)(stats + (size_t)M * sp.splits);
+    for (int t0 = 0; t0 < M; t0 += MAX_GRID_ROWS) {
+        const int rows = min(MAX_GRID_ROWS, M - t0);
+        const LogprobsOut r{logits + (size_t)t0 * V, tokens ? tokens + t0 : nullptr, logprob_out ? logprob_out + t0 : nullptr,
+                            entropy_out ? entropy_out + t0 : nullptr, top_out ? top_out + (size_t)t0 * top_k : nullptr,
+                            top_logprob_out ? top_logprob_out + (size_t)t0 * top_k : nullptr};
+        k_logprobs<<<dim3(sp.splits, rows), ROW_NT, 0, st>>>(r, V, sp.range, invT, top_k, stats, tops);
+        HIP_TRY(hipGetLastError());
+        if (sp.splits > 1) {
+            k_logprobs_join<<<rows, ROW_NT, 0, st>>>(r, V, sp.splits, invT, top_k, stats, tops);
+            HIP_TRY(hipGetLastError());
+        }
+    }
     return PETALS_OK;
 }
 
@@ -460,9 +646,20 @@ int petals_client_distill(petals_client *client, const float *logits, int32_t M,
     if (K > PETALS_DISTILL_TOP_MAX) return ps_fail(PETALS_ERR_UNSUPPORTED, "K %d exceeds %d", K, PETALS_DISTILL_TOP_MAX);
     if (!loss_out && !grad_logits_out) return ps_fail(PETALS_ERR_INVALID_ARG, "neither loss nor gradient requested");
     if (!usable_temperature(temperature)) return ps_fail(PETALS_ERR_INVALID_ARG, "temperature must be positive and finite");
-    k_distill<<<M, ROW_NT, 0, (hipStream_t)stream>>>(logits, c.cfg->vocab, teacher_tokens, teacher_logits, K, temperature, loss_grad, loss_out,
-                                                     grad_logits_out);
-    HIP_TRY(hipGetLastError());
+    hipStream_t st = (hipStream_t)stream;
+    const int V = c.cfg->vocab;
+    const RowSplit sp = row_split(M, V, (int)min((size_t)1 << 20, c.scratch_bytes / ((size_t)M * sizeof(DistillPart))));
+    DistillPart *parts = (DistillPart *)c.scratch;
+    for (int t0 = 0; t0 < M; t0 += MAX_GRID_ROWS) {
+        const int rows = min(MAX_GRID_ROWS, M - t0);
+        const DistillIn d{logits + (size_t)t0 * V, teacher_tokens + (size_t)t0 * K, teacher_logits + (size_t)t0 * K,
+                          loss_grad ? loss_grad + t0 : nullptr, loss_out ? loss_out + t0 : nullptr,
+                          grad_logits_out ? grad_logits_out + (size_t)t0 * V : nullptr, V, K, (double)temperature, 1.0 / (double)temperature};
+        k_distill_stats<<<dim3(sp.splits, rows), ROW_NT, 0, st>>>(d, sp.range, parts);
+        HIP_TRY(hipGetLastError());
+        k_distill_grad<<<dim3(grad_logits_out ? sp.splits : 1, rows), ROW_NT, 0, st>>>(d, sp.range, sp.splits, parts);
+        HIP_TRY(hipGetLastError());
+    }
     return PETALS_OK;
 }
 
