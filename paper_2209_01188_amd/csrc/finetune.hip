@@ -9,6 +9,15 @@
 #include "host_util.h"
 #include "ln_backward.h"
 
+#ifndef DGB
+#define DGB 96
+#endif
+#ifndef PREF
+#define PREF 1
+#endif
+#ifndef RG
+#define RG 1024
+#endif
 namespace {
 
 // ------------------------------------------------------------------------------------ a row's softmax statistics
@@ -23,13 +32,36 @@ struct RowStat {
     float m;
     double S, D;
 };
-__device__ __forceinline__ RowStat merge(const RowStat &a, const RowStat &b, double invT) {
-    const float m = fmaxf(a.m, b.m);
-    if (m == -INFINITY) return RowStat{m, a.S + b.S, a.D + b.D};        // (sums of nothing, or NaN)
-    const double ta = ((double)a.m - m) * invT, tb = ((double)b.m - m) * invT, ea = exp_f64(ta), eb = exp_f64(tb);
-    // a part without any logit above -infinity: S = D = 0, and its t is no number to multiply with
-    const double da = a.m == -INFINITY ? 0.0 : ea * fma(ta / LN2, a.S, a.D), db = b.m == -INFINITY ? 0.0 : eb * fma(tb / LN2, b.S, b.D);
-    return RowStat{m, ea * a.S + eb * b.S, da + db};
+// s in terms of a maximum m that is at least its own.  (A part without any logit above -infinity: S = D = 0, or NaN, and its
+// distance to m is no number to multiply with.)
+__device__ __forceinline__ void rescale(RowStat &s, float m, double invT) {
+    if (s.m != -INFINITY) {
+        const double t = ((double)s.m - m) * invT, e = exp_f64(t);
+        s.D = e * fma(t / LN2, s.S, s.D);
+        s.S *= e;
+    }
+    s.m = m;
+}
+__device__ __forceinline__ void merge(RowStat &s, RowStat o, double invT) {
+    const float m = fmaxf(s.m, o.m);
+    rescale(s, m, invT);
+    rescale(o, m, invT);
+    s.S += o.S;
+    s.D += o.D;
+}
+__device__ __forceinline__ RowStat wave_merge(RowStat s, double invT) {
+    rescale(s, wave_max(s.m), invT);
+    return RowStat{s.m, wave_sum(s.S), wave_sum(s.D)};
+}
+// over the workgroup, in a fixed order; every thread gets it.  sm: NW of them
+template <int NW>
+__device__ __forceinline__ RowStat block_merge(RowStat s, double invT, RowStat *sm) {
+    s = wave_merge(s, invT);
+    const int lane = threadIdx.x & 63;
+    if (lane == 0) sm[threadIdx.x >> 6] = s;
+    __syncthreads();
+    s = lane < NW ? sm[lane] : RowStat{-INFINITY, 0.0, 0.0};
+    return wave_merge(s, invT);
 }
 // N further logits of a thread; returns the largest of them
 template <int N, bool WITH_D>
@@ -37,14 +69,7 @@ __device__ __forceinline__ float accumulate(RowStat &s, const float (&l)[N], flo
     float cm = l[0];
 #pragma unroll
     for (int i = 1; i < N; i++) cm = fmaxf(cm, l[i]);
-    if (cm > s.m) {
-        if (s.m != -INFINITY) {
-            const double t = ((double)s.m - cm) * invT, e = exp_f64(t);
-            if (WITH_D) s.D = e * fma(t / LN2, s.S, s.D);
-            s.S *= e;
-        }
-        s.m = cm;
-    }
+    if (cm > s.m) rescale(s, cm, invT);
     const float m = s.m == -INFINITY ? 0.0f : s.m;
 #pragma unroll
     for (int i = 0; i < N; i++) {
@@ -54,30 +79,11 @@ __device__ __forceinline__ float accumulate(RowStat &s, const float (&l)[N], flo
     }
     return cm;
 }
-__device__ __forceinline__ RowStat shfl_xor(const RowStat &s, int off) {
-    return RowStat{__shfl_xor(s.m, off), __shfl_xor(s.S, off), __shfl_xor(s.D, off)};
-}
-// over the workgroup, in a fixed order; every thread gets it
-template <int NW>
-__device__ __forceinline__ RowStat block_merge(RowStat s, double invT, RowStat *sm) {
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const RowStat o = shfl_xor(s, off);
-        s = (threadIdx.x & off) ? merge(o, s, invT) : merge(s, o, invT);
-    }
-    if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = s;
-    __syncthreads();
-    RowStat r = sm[0];
-#pragma unroll
-    for (int w = 1; w < NW; w++) r = merge(r, sm[w], invT);
-    __syncthreads();
-    return r;
-}
 
 constexpr int ROW_NT = 256, ROW_NW = ROW_NT / 64;
 constexpr int ROW_PER = 16;                         // logits of a thread per step
 constexpr int WAVE_STEP = 64 * ROW_PER, ROW_STEP = ROW_NW * WAVE_STEP;
-constexpr int ROW_GROUPS = 2048;                    // workgroups that fill the chip: 8 per compute unit
+constexpr int ROW_GROUPS = RG;                    // workgroups that keep the memory busy: 4 per compute unit
 typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));     // rows of an odd vocabulary begin anywhere
 
 // A call of few rows shares each row out over workgroups, a whole number of steps to each.
@@ -85,24 +91,48 @@ struct RowSplit {
     int splits, range;
 };
 RowSplit row_split(int M, int V, int most) {
-    const int steps = (V + ROW_STEP - 1) / ROW_STEP, want = max(1, min(most, (ROW_GROUPS + M - 1) / M)), per = (steps + min(steps, want) - 1) / min(steps, want);
+    const int steps = (V + ROW_STEP - 1) / ROW_STEP, want = max(1, min(min(steps, most), (ROW_GROUPS + M - 1) / M)), per = (steps + want - 1) / want;
     return RowSplit{(steps + per - 1) / per, per * ROW_STEP};
 }
 
-// logit 4 q + e of a thread's step is column first + 256 q + e, first = the wave's first column + 4 lane; what lies behind the row is -infinity
-__device__ __forceinline__ void load_logits(const float *__restrict__ row, int first, int end, float (&l)[ROW_PER]) {
+// logit 4 q + e of a thread's step is column v0 + 256 q + 4 lane + e, v0 = the wave's first; what lies behind the row is -infinity
+__device__ __forceinline__ void load_logits(const float *row, int v0, int end, float (&l)[ROW_PER]) {
+    const int first = v0 + 4 * (threadIdx.x & 63);
+    if (v0 + WAVE_STEP <= end) {
 #pragma unroll
-    for (int q = 0; q < ROW_PER / 4; q++) {
-        const int v = first + 256 * q;
-        if (v + 3 < end) {
-            const v4f f = *(const v4f_any *)(row + v);
+        for (int q = 0; q < ROW_PER / 4; q++) {
+            const v4f f = *(const v4f_any *)(row + first + 256 * q);
 #pragma unroll
             for (int e = 0; e < 4; e++) l[4 * q + e] = f[e];
-        } else {
+        }
+    } else {
 #pragma unroll
-            for (int e = 0; e < 4; e++) l[4 * q + e] = v + e < end ? row[v + e] : -INFINITY;
+        for (int i = 0; i < ROW_PER; i++) {
+            const int v = first + 256 * (i >> 2) + (i & 3);
+            l[i] = v < end ? row[v] : -INFINITY;
         }
     }
+}
+// the steps of this wave in [begin, end), the next one's logits on their way while one is worked on: step(first column, logits)
+template <typename F>
+__device__ __forceinline__ void walk_row(const float *row, int begin, int end, F step) {
+#if PREF
+    float l[ROW_PER], ahead[ROW_PER];
+    int v = begin + (threadIdx.x >> 6) * WAVE_STEP;
+    if (v < end) load_logits(row, v, end, l);
+    for (; v < end; v += ROW_STEP) {
+        if (v + ROW_STEP < end) load_logits(row, v + ROW_STEP, end, ahead);
+        step(v, l);
+#pragma unroll
+        for (int i = 0; i < ROW_PER; i++) l[i] = ahead[i];
+    }
+#else
+    for (int v = begin + (threadIdx.x >> 6) * WAVE_STEP; v < end; v += ROW_STEP) {
+        float l[ROW_PER];
+        load_logits(row, v, end, l);
+        step(v, l);
+    }
+#endif
 }
 
 // ------------------------------------------------------------------------------------ the largest logits of a row
@@ -124,10 +154,6 @@ __device__ __forceinline__ uint64_t read_lane(uint64_t v, int lane) {
 }
 struct TopList {
     uint64_t key = 0, last = 0;         // this lane's key; the one at place top_k - 1
-    __device__ __forceinline__ void start(uint64_t k, int top_k) {        // a list that is in order already
-        key = k;
-        last = read_lane(key, top_k - 1);
-    }
     __device__ __forceinline__ void offer(uint64_t k, int top_k) {        // one key per lane, 0: none
         const int lane = threadIdx.x & 63;
         unsigned long long who = __ballot(k > last);
@@ -167,12 +193,13 @@ __device__ __forceinline__ void logprobs_store(const LogprobsOut &o, int t, int 
     }
 }
 // the waves' lists become the first wave's
+template <int NW>
 __device__ __forceinline__ void join_lists(TopList &list, uint64_t (*lists)[64], int top_k) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     lists[wave][lane] = list.key;
     __syncthreads();
     if (wave == 0)
-        for (int w = 1; w < ROW_NW; w++) list.offer(lists[w][lane], top_k);
+        for (int w = 1; w < NW; w++) list.offer(lists[w][lane], top_k);
 }
 
 // workgroup (split, row): the split's part of the row, and with one split the results
@@ -180,17 +207,11 @@ __global__ void __launch_bounds__(ROW_NT) k_logprobs(LogprobsOut o, int V, int r
                                                      uint64_t *__restrict__ tops) {
     __shared__ RowStat sm[ROW_NW];
     __shared__ uint64_t lists[ROW_NW][64];
-    const int t = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const float *row = o.logits + (size_t)t * V;
+    const int t = blockIdx.y, lane = threadIdx.x & 63, begin = blockIdx.x * range, end = min(V, begin + range);
     const float c = (float)(invT / LN2);
-    const int end = min(V, ((int)blockIdx.x + 1) * range);
     RowStat s{-INFINITY, 0.0, 0.0};
     TopList list;
-    int v0 = blockIdx.x * range + wave * WAVE_STEP;
-    float l[ROW_PER], ahead[ROW_PER];
-    if (v0 < end) load_logits(row, v0 + 4 * lane, end, l);
-    for (; v0 < end; v0 += ROW_STEP) {
-        if (v0 + ROW_STEP < end) load_logits(row, v0 + ROW_STEP + 4 * lane, end, ahead);
+    walk_row(o.logits + (size_t)t * V, begin, end, [&](int v0, const float (&l)[ROW_PER]) {
         const float most = accumulate<ROW_PER, true>(s, l, c, invT);
         if (top_k && __ballot(!(most < key_value(list.last)))) {
 #pragma unroll
@@ -199,11 +220,9 @@ __global__ void __launch_bounds__(ROW_NT) k_logprobs(LogprobsOut o, int V, int r
                 list.offer(v < end ? (uint64_t)order_key(l[i]) << 32 | (uint32_t)~v : 0, top_k);
             }
         }
-#pragma unroll
-        for (int i = 0; i < ROW_PER; i++) l[i] = ahead[i];
-    }
+    });
     s = block_merge<ROW_NW>(s, invT, sm);
-    if (top_k) join_lists(list, lists, top_k);
+    if (top_k) join_lists<ROW_NW>(list, lists, top_k);
     if (gridDim.x == 1) {
         logprobs_store(o, t, V, invT, top_k, s, list);
         return;
@@ -214,210 +233,204 @@ __global__ void __launch_bounds__(ROW_NT) k_logprobs(LogprobsOut o, int V, int r
 }
 
 // what the splits of a row have found
-__global__ void __launch_bounds__(ROW_NT) k_logprobs_join(LogprobsOut o, int V, int splits, double invT, int top_k,
-                                                          const RowStat *__restrict__ stats, const uint64_t *__restrict__ tops) {
-    __shared__ RowStat sm[ROW_NW];
-    __shared__ uint64_t lists[ROW_NW][64];
-    const int t = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+constexpr int JOIN_NT = 1024, JOIN_NW = JOIN_NT / 64;
+__global__ void __launch_bounds__(JOIN_NT) k_logprobs_join(LogprobsOut o, int V, int splits, double invT, int top_k,
+                                                           const RowStat *__restrict__ stats, const uint64_t *__restrict__ tops) {
+    __shared__ RowStat sm[JOIN_NW];
+    __shared__ uint64_t lists[JOIN_NW][64];
+    const int t = blockIdx.x, n = splits * top_k;
     RowStat s{-INFINITY, 0.0, 0.0};
-    for (int i = threadIdx.x; i < splits; i += ROW_NT) s = merge(s, stats[(size_t)t * splits + i], invT);
-    s = block_merge<ROW_NW>(s, invT, sm);
+    for (int i = threadIdx.x; i < splits; i += JOIN_NT) merge(s, stats[(size_t)t * splits + i], invT);
     TopList list;
-    if (top_k) {
-        for (int i = wave; i < splits; i += ROW_NW) {
-            const uint64_t k = lane < top_k ? tops[((size_t)t * splits + i) * top_k + lane] : 0;
-            if (i == wave) list.start(k, top_k);
-            else list.offer(k, top_k);
-        }
-        join_lists(list, lists, top_k);
-    }
+    const uint64_t *keys = tops + (size_t)t * n;
+    for (int i = threadIdx.x; i < (n + 63) / 64 * 64; i += JOIN_NT) list.offer(i < n ? keys[i] : 0, top_k);
+    s = block_merge<JOIN_NW>(s, invT, sm);
+    if (top_k) join_lists<JOIN_NW>(list, lists, top_k);
     logprobs_store(o, t, V, invT, top_k, s, list);
 }
 
 // ------------------------------------------------------------------------------------ distillation
 //
-// Two passes over the logits, the softmax statistics and then w q, in launches of their own for calls of few rows, whose rows
-// are shared out over workgroups.  With x = z / T - max / T, log q = x - log S, so a part of the list (the entries whose
-// tokens lie in a workgroup's range) adds sum p (log p - z / T) and sum p to the loss, and the rest is the row's alone.
-struct DistillPart {
-    float m;
-    double S, term, mass;
-};
+// Two passes over the logits: the softmax statistics, then w q.  A call goes through its rows in groups whose logits fit the
+// cache in front of the memory, so that the second pass need not ask the memory again: launch k takes the first pass of
+// group k and the second of group k - 1, whose reads and writes then share the launch.
 struct DistillIn {
     const float *logits;
     const int32_t *ids;
     const float *vals;
     const float *loss_grad;
     float *loss, *grad;
-    int V, K;
+    int V, K, range;
     double T, invT;
 };
-constexpr int LIST_PER = (PETALS_DISTILL_TOP_MAX + ROW_NT - 1) / ROW_NT;
-struct Teacher {                       // entry k = i ROW_NT + threadIdx.x; id -1: none
-    int id[LIST_PER];
-    double p[LIST_PER], logp[LIST_PER];
-    bool listed;
+struct DistillPart {                   // of a row and split
+    float m;
+    double S;
 };
-template <int NT>
-__device__ __forceinline__ void teacher_row(const DistillIn &d, int t, Teacher &te, float *sf, double *sd) {
-    float val[LIST_PER], mx = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < LIST_PER; i++) {
-        const int k = i * NT + threadIdx.x;
-        te.id[i] = -1;
-        val[i] = -INFINITY;
-        if (k < d.K) {
-            const int id = d.ids[(size_t)t * d.K + k];
-            if (id >= 0 && id < d.V) {
-                te.id[i] = id;
-                val[i] = d.vals[(size_t)t * d.K + k];
-            }
-        }
-        mx = fmaxf(mx, val[i]);
-    }
-    mx = block_max<NT / 64>(mx, sf);
-    double sum = 0.0;
-#pragma unroll
-    for (int i = 0; i < LIST_PER; i++) {
-        te.logp[i] = ((double)val[i] - mx) * d.invT;
-        te.p[i] = val[i] == -INFINITY ? 0.0 : exp_f64(te.logp[i]);
-        sum += te.p[i];
-    }
-    sum = block_sum<NT / 64>(sum, sd);
-    te.listed = !(sum == 0.0);                             // (or NaN)
-    const double ls = log(sum);
-#pragma unroll
-    for (int i = 0; i < LIST_PER; i++) {
-        te.p[i] /= sum;
-        te.logp[i] -= ls;
-    }
+struct DistillRow {                    // of a row, by the workgroup of its first split
+    double max, norm;                  // of the teacher's logits, and 1 / sum of e^((logit - max) / T)
+    double term, mass;                 // sum p (log p - z / T) and sum p: with log q = z / T - lse the loss is T^2 (term + mass lse)
+    int listed;
+};
+constexpr int LIST_PER = (PETALS_DISTILL_TOP_MAX + ROW_NT - 1) / ROW_NT;
+
+// entry k of a row's list; an entry that counts for nothing has value -infinity
+__device__ __forceinline__ float teacher_entry(const DistillIn &d, int t, int k, int &id) {
+    id = -1;
+    if (k >= d.K) return -INFINITY;
+    id = d.ids[(size_t)t * d.K + k];
+    if (id < 0 || id >= d.V) id = -1;
+    return id < 0 ? -INFINITY : d.vals[(size_t)t * d.K + k];
 }
 
-// workgroup (split, row)
-__global__ void __launch_bounds__(ROW_NT) k_distill_stats(DistillIn d, int range, DistillPart *__restrict__ parts) {
-    __shared__ RowStat sm[ROW_NW];
-    __shared__ double sd[ROW_NW];
-    __shared__ float sf[ROW_NW];
-    const int t = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+__device__ __forceinline__ void distill_stats(const DistillIn &d, int t, DistillPart *__restrict__ part, DistillRow *__restrict__ out,
+                                              RowStat *sm, double *sd, float *sf) {
     const float *row = d.logits + (size_t)t * d.V;
     const float c = (float)(d.invT / LN2);
-    const int begin = blockIdx.x * range, end = min(d.V, begin + range);
-    Teacher te;
-    teacher_row<ROW_NT>(d, t, te, sf, sd);
-    if (!te.listed) return;                                // nobody reads the part
-    double term = 0.0, mass = 0.0;
+    const int begin = blockIdx.x * d.range, end = min(d.V, begin + d.range);
+    float val[LIST_PER], mx = -INFINITY;
+    int id[LIST_PER];
+    bool some = false;
 #pragma unroll
-    for (int i = 0; i < LIST_PER; i++)
-        if (te.id[i] >= begin && te.id[i] < end && !(te.p[i] == 0.0)) {
-            term += te.p[i] * (te.logp[i] - (double)row[te.id[i]] * d.invT);
-            mass += te.p[i];
-        }
-    RowStat s{-INFINITY, 0.0, 0.0};
-    int v0 = begin + wave * WAVE_STEP;
-    float l[ROW_PER], ahead[ROW_PER];
-    if (v0 < end) load_logits(row, v0 + 4 * lane, end, l);
-    for (; v0 < end; v0 += ROW_STEP) {
-        if (v0 + ROW_STEP < end) load_logits(row, v0 + ROW_STEP + 4 * lane, end, ahead);
-        accumulate<ROW_PER, false>(s, l, c, d.invT);
-#pragma unroll
-        for (int i = 0; i < ROW_PER; i++) l[i] = ahead[i];
+    for (int i = 0; i < LIST_PER; i++) {
+        val[i] = -INFINITY;
+        id[i] = -1;
+        if (i * ROW_NT < d.K) val[i] = teacher_entry(d, t, i * ROW_NT + threadIdx.x, id[i]);
+        mx = fmaxf(mx, val[i]);
+        some |= !(val[i] == -INFINITY);
     }
+    const bool listed = __syncthreads_or(some);
+    if (blockIdx.x == 0) {
+        DistillRow r{0.0, 0.0, 0.0, 0.0, listed};
+        if (listed) {
+            mx = block_max<ROW_NW>(mx, sf);
+            double sum = 0.0, term = 0.0, mass = 0.0;
+#pragma unroll
+            for (int i = 0; i < LIST_PER; i++)
+                if (i * ROW_NT < d.K) sum += val[i] == -INFINITY ? 0.0 : exp_f64(((double)val[i] - mx) * d.invT);
+            sum = block_sum<ROW_NW>(sum, sd);
+            const double ls = log(sum);
+#pragma unroll
+            for (int i = 0; i < LIST_PER; i++) {
+                if (val[i] == -INFINITY) continue;
+                const double tt = ((double)val[i] - mx) * d.invT, p = exp_f64(tt) / sum;
+                if (!(p == 0.0)) {
+                    term += p * (tt - ls - (double)row[id[i]] * d.invT);
+                    mass += p;
+                }
+            }
+            term = block_sum<ROW_NW>(term, sd);
+            mass = block_sum<ROW_NW>(mass, sd);
+            r = DistillRow{(double)mx, 1.0 / sum, term, mass, 1};
+        }
+        if (threadIdx.x == 0) *out = r;
+    }
+    if (!listed) return;                                   // nobody reads the part
+    RowStat s{-INFINITY, 0.0, 0.0};
+    walk_row(row, begin, end, [&](int, const float (&l)[ROW_PER]) { accumulate<ROW_PER, false>(s, l, c, d.invT); });
     s = block_merge<ROW_NW>(s, d.invT, sm);
-    term = block_sum<ROW_NW>(term, sd);
-    mass = block_sum<ROW_NW>(mass, sd);
-    if (threadIdx.x == 0) parts[(size_t)t * gridDim.x + blockIdx.x] = DistillPart{s.m, s.S, term, mass};
+    if (threadIdx.x == 0) *part = DistillPart{s.m, s.S};
 }
 
 // The gradient of a workgroup's range (logits and gradient may be the same memory: what a thread overwrites it has read, and
-// other threads' logits it reads before the barrier), and by the first workgroup of the row its loss.  The list's columns get
+// the list's logits are read before the barrier), and by the first workgroup of the row its loss.  The list's columns get
 // theirs, w (q - p) in fp64, after the others.
-__global__ void __launch_bounds__(ROW_NT) k_distill_grad(DistillIn d, int range, int splits, const DistillPart *__restrict__ parts) {
+__device__ __forceinline__ void distill_grad(const DistillIn &d, int t, const DistillPart *__restrict__ parts, const DistillRow *__restrict__ rows,
+                                             int *s_id, double *s_p) {
+    const int lane = threadIdx.x & 63, splits = gridDim.x;
+    const float *row = d.logits + (size_t)t * d.V;
+    const float c = (float)(d.invT / LN2);
+    const int begin = blockIdx.x * d.range, end = min(d.V, begin + d.range);
+    if (!d.grad && blockIdx.x) return;
+    const DistillRow r = rows[t];
+    RowStat s{-INFINITY, 0.0, 0.0};
+    if (r.listed) {
+        for (int i = lane; i < splits; i += 64) {          // by every wave
+            const DistillPart p = parts[(size_t)t * splits + i];
+            merge(s, RowStat{p.m, p.S, 0.0}, d.invT);
+        }
+        s = wave_merge(s, d.invT);
+    }
+    const bool none = s.S == 0.0, zero = !r.listed || none;
+    if (blockIdx.x == 0 && threadIdx.x == 0 && d.loss)
+        d.loss[t] = !r.listed ? 0.0f : none ? INFINITY : (float)(d.T * d.T * (r.term + r.mass * ((double)s.m * d.invT + log(s.S))));
+    if (!d.grad) return;
+    float *out = d.grad + (size_t)t * d.V;
+    const double w = d.T * (d.loss_grad ? (double)d.loss_grad[t] : 1.0);
+    int id[LIST_PER];
+    float at[LIST_PER];
+    if (!zero) {
+        bool mine = false;
+#pragma unroll
+        for (int i = 0; i < LIST_PER; i++) {
+            id[i] = -1;
+            const int k = i * ROW_NT + threadIdx.x;
+            if (i * ROW_NT < d.K) {
+                const float val = teacher_entry(d, t, k, id[i]);
+                if (k < d.K) {
+                    s_id[k] = id[i];
+                    s_p[k] = val == -INFINITY ? 0.0 : exp_f64(((double)val - r.max) * d.invT) * r.norm;
+                }
+                if (id[i] < begin || id[i] >= end) id[i] = -1;
+                mine |= id[i] >= 0;
+            }
+        }
+        __syncthreads();
+        if (mine) {
+#pragma unroll
+            for (int i = 0; i < LIST_PER; i++) {
+                if (id[i] < 0) continue;
+                double p = 0.0;
+                for (int j = 0; j < d.K; j++) p += s_id[j] == id[i] ? s_p[j] : 0.0;
+                at[i] = (float)(w * (exp_f64(((double)row[id[i]] - s.m) * d.invT) / s.S - p));
+            }
+        }
+        __syncthreads();
+    }
+    const float f = zero ? 0.0f : (float)(w / s.S), m = s.m;
+    const auto store = [&](int v0, const float (&g)[ROW_PER]) {
+        if (v0 + WAVE_STEP <= end) {
+#pragma unroll
+            for (int q = 0; q < ROW_PER / 4; q++)
+                __builtin_nontemporal_store(v4f{g[4 * q], g[4 * q + 1], g[4 * q + 2], g[4 * q + 3]}, (v4f_any *)(out + v0 + 4 * lane + 256 * q));
+        } else {
+#pragma unroll
+            for (int i = 0; i < ROW_PER; i++) {
+                const int v = v0 + 4 * lane + 256 * (i >> 2) + (i & 3);
+                if (v < end) out[v] = g[i];
+            }
+        }
+    };
+    if (zero) {
+        const float g[ROW_PER] = {};
+        for (int v0 = begin + (threadIdx.x >> 6) * WAVE_STEP; v0 < end; v0 += ROW_STEP) store(v0, g);
+        return;
+    }
+    walk_row(row, begin, end, [&](int v0, const float (&l)[ROW_PER]) {
+        float g[ROW_PER];
+#pragma unroll
+        for (int i = 0; i < ROW_PER; i++) g[i] = f * __builtin_amdgcn_exp2f((l[i] - m) * c);
+        store(v0, g);
+    });
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < LIST_PER; i++)
+        if (id[i] >= 0) out[id[i]] = at[i];                // (entries with the same token write the same)
+}
+
+// workgroup (split, row): rows [first2, first2 + n2) their second pass, the others, from row first1 on, their first
+__global__ void __launch_bounds__(ROW_NT) k_distill(DistillIn d, int first2, int n2, int first1, DistillPart *__restrict__ parts,
+                                                    DistillRow *__restrict__ rows) {
     __shared__ RowStat sm[ROW_NW];
     __shared__ double sd[ROW_NW];
     __shared__ float sf[ROW_NW];
     __shared__ int s_id[PETALS_DISTILL_TOP_MAX];
     __shared__ double s_p[PETALS_DISTILL_TOP_MAX];
-    const int t = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const float *row = d.logits + (size_t)t * d.V;
-    const float c = (float)(d.invT / LN2);
-    const int begin = blockIdx.x * range, end = min(d.V, begin + range);
-    Teacher te;
-    teacher_row<ROW_NT>(d, t, te, sf, sd);
-    RowStat s{-INFINITY, 0.0, 0.0};
-    double term = 0.0, mass = 0.0;
-    if (te.listed) {
-        for (int i = threadIdx.x; i < splits; i += ROW_NT) {
-            const DistillPart p = parts[(size_t)t * splits + i];
-            s = merge(s, RowStat{p.m, p.S, 0.0}, d.invT);
-            term += p.term;
-            mass += p.mass;
-        }
-    }
-    s = block_merge<ROW_NW>(s, d.invT, sm);
-    const bool none = s.S == 0.0;
-    if (blockIdx.x == 0 && d.loss) {
-        term = block_sum<ROW_NW>(term, sd);
-        mass = block_sum<ROW_NW>(mass, sd);
-        if (threadIdx.x == 0)
-            d.loss[t] = !te.listed ? 0.0f : none ? INFINITY : (float)(d.T * d.T * (term + mass * ((double)s.m * d.invT + log(s.S))));
-    }
-    if (!d.grad) return;
-    float *out = d.grad + (size_t)t * d.V;
-    const bool zero = !te.listed || none;
-    const double w = d.T * (d.loss_grad ? (double)d.loss_grad[t] : 1.0);
-    bool mine = false;
-#pragma unroll
-    for (int i = 0; i < LIST_PER; i++) {
-        const int k = i * ROW_NT + threadIdx.x;
-        if (k < d.K) {
-            s_id[k] = te.id[i];
-            s_p[k] = te.p[i];
-        }
-        if (zero || te.id[i] < begin || te.id[i] >= end) te.id[i] = -1;
-        mine |= te.id[i] >= 0;
-    }
-    __syncthreads();
-    float at[LIST_PER];
-    if (mine) {
-#pragma unroll
-        for (int i = 0; i < LIST_PER; i++) {
-            if (te.id[i] < 0) continue;
-            double p = 0.0;
-            for (int j = 0; j < d.K; j++) p += s_id[j] == te.id[i] ? s_p[j] : 0.0;
-            at[i] = (float)(w * (exp_f64(((double)row[te.id[i]] - s.m) * d.invT) / s.S - p));
-        }
-    }
-    __syncthreads();
-    const float f = zero ? 0.0f : (float)(w / s.S), m = zero ? 0.0f : s.m;
-    int v0 = begin + wave * WAVE_STEP;
-    float l[ROW_PER], ahead[ROW_PER];
-#pragma unroll
-    for (int i = 0; i < ROW_PER; i++) l[i] = ahead[i] = 0.0f;
-    if (v0 < end && !zero) load_logits(row, v0 + 4 * lane, end, l);
-    for (; v0 < end; v0 += ROW_STEP) {
-        if (v0 + ROW_STEP < end && !zero) load_logits(row, v0 + ROW_STEP + 4 * lane, end, ahead);
-#pragma unroll
-        for (int q = 0; q < ROW_PER / 4; q++) {
-            const int v = v0 + 4 * lane + 256 * q;
-            v4f g;
-#pragma unroll
-            for (int e = 0; e < 4; e++) g[e] = zero ? 0.0f : f * __builtin_amdgcn_exp2f((l[4 * q + e] - m) * c);
-            if (v + 3 < end) {
-                __builtin_nontemporal_store(g, (v4f_any *)(out + v));
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; e++)
-                    if (v + e < end) out[v + e] = g[e];
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < ROW_PER; i++) l[i] = ahead[i];
-    }
-    __syncthreads();
-    if (mine) {
-#pragma unroll
-        for (int i = 0; i < LIST_PER; i++)
-            if (te.id[i] >= 0) out[te.id[i]] = at[i];      // (entries with the same token write the same)
+    if ((int)blockIdx.y < n2) {
+        distill_grad(d, first2 + (int)blockIdx.y, parts, rows, s_id, s_p);
+    } else {
+        const int t = first1 + (int)blockIdx.y - n2;
+        distill_stats(d, t, parts + (size_t)t * gridDim.x + blockIdx.x, rows + t, sm, sd, sf);
     }
 }
 
@@ -592,7 +605,8 @@ int check_call(const petals_client_config &cfg, int32_t M) {
     if (M > cfg.max_rows_per_call) return ps_fail(PETALS_ERR_CAPACITY, "%d rows exceed max_rows_per_call %d", M, cfg.max_rows_per_call);
     return PETALS_OK;
 }
-constexpr int MAX_GRID_ROWS = 1 << 15;      // rows of one launch (the grid's second dimension)
+constexpr int MAX_GRID_ROWS = 1 << 14;      // rows of a group (two groups share the grid's second dimension)
+constexpr size_t DISTILL_GROUP_BYTES = (size_t)DGB << 20;
 bool usable_temperature(float t) { return t > 0.0f && t < INFINITY && 1.0f / t < INFINITY; }
 
 }  // namespace
@@ -629,7 +643,7 @@ int petals_client_logprobs(petals_client *client, const float *logits, const int
         k_logprobs<<<dim3(sp.splits, rows), ROW_NT, 0, st>>>(r, V, sp.range, invT, top_k, stats, tops);
         HIP_TRY(hipGetLastError());
         if (sp.splits > 1) {
-            k_logprobs_join<<<rows, ROW_NT, 0, st>>>(r, V, sp.splits, invT, top_k, stats, tops);
+            k_logprobs_join<<<rows, JOIN_NT, 0, st>>>(r, V, sp.splits, invT, top_k, stats, tops);
             HIP_TRY(hipGetLastError());
         }
     }
@@ -648,17 +662,17 @@ int petals_client_distill(petals_client *client, const float *logits, int32_t M,
     if (!usable_temperature(temperature)) return ps_fail(PETALS_ERR_INVALID_ARG, "temperature must be positive and finite");
     hipStream_t st = (hipStream_t)stream;
     const int V = c.cfg->vocab;
-    const RowSplit sp = row_split(M, V, (int)min((size_t)1 << 20, c.scratch_bytes / ((size_t)M * sizeof(DistillPart))));
-    DistillPart *parts = (DistillPart *)c.scratch;
-    for (int t0 = 0; t0 < M; t0 += MAX_GRID_ROWS) {
-        const int rows = min(MAX_GRID_ROWS, M - t0);
-        const DistillIn d{logits + (size_t)t0 * V, teacher_tokens + (size_t)t0 * K, teacher_logits + (size_t)t0 * K,
-                          loss_grad ? loss_grad + t0 : nullptr, loss_out ? loss_out + t0 : nullptr,
-                          grad_logits_out ? grad_logits_out + (size_t)t0 * V : nullptr, V, K, (double)temperature, 1.0 / (double)temperature};
-        k_distill_stats<<<dim3(sp.splits, rows), ROW_NT, 0, st>>>(d, sp.range, parts);
+    DistillRow *rows = (DistillRow *)c.scratch;
+    DistillPart *parts = (DistillPart *)(rows + M);
+    const int group = grad_logits_out ? (int)max((size_t)1, min((size_t)MAX_GRID_ROWS, DISTILL_GROUP_BYTES / ((size_t)V * sizeof(float)))) : MAX_GRID_ROWS;
+    const size_t room = (c.scratch_bytes - sizeof(DistillRow) * M) / ((size_t)M * sizeof(DistillPart));
+    const RowSplit sp = row_split(min(M, group), V, (int)min((size_t)1 << 20, room));
+    const DistillIn d{logits, teacher_tokens, teacher_logits, loss_grad, loss_out, grad_logits_out, V, K, sp.range, (double)temperature, 1.0 / (double)temperature};
+    for (int t0 = 0, n2 = 0; t0 < M || n2; t0 += group) {
+        const int n1 = max(0, min(group, M - t0));
+        k_distill<<<dim3(sp.splits, n2 + n1), ROW_NT, 0, st>>>(d, t0 - group, n2, t0, parts, rows);
         HIP_TRY(hipGetLastError());
-        k_distill_grad<<<dim3(grad_logits_out ? sp.splits : 1, rows), ROW_NT, 0, st>>>(d, sp.range, sp.splits, parts);
-        HIP_TRY(hipGetLastError());
+        n2 = n1;
     }
     return PETALS_OK;
 }
