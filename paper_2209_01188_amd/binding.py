@@ -47,6 +47,12 @@ def lib():
         for name in EXPORTS + CLIENT_EXPORTS + FINETUNE_EXPORTS:
             if name != "petals_last_error":
                 getattr(L, name).restype = C.c_int
+        P, I, F = C.c_void_p, C.c_int32, C.c_float
+        L.petals_client_logprobs.argtypes = [P, P, P, I, F, I, P, P, P, P, P]
+        L.petals_client_distill.argtypes = [P, P, I, P, P, I, F, P, P, P, P]
+        L.petals_client_lm_head_backward_bytes.argtypes = [P, I, P]
+        L.petals_client_lm_head_backward.argtypes = [P, P, P, P, I, P, P]
+        L.petals_client_embed_backward.argtypes = [P, P, P, I, P, P, P, P]
         _lib = L
     return _lib
 
@@ -481,32 +487,41 @@ def petals_client_sample(client, logits, temperature, top_k, uniforms, next_toke
 
 # scoring and the client's ends of a fine-tuning step (petals_finetune.h)
 
+# Serving and training call these in a loop beside small kernels: argument types are declared once (in lib()), so that
+# plain integers go through without a ctypes object each.
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+def _raw_stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
 def petals_client_logprobs(client, logits, tokens, temperature, top_k, logprob_out, entropy_out, top_out, top_logprob_out):
-    _check(lib().petals_client_logprobs(client, _ptr(logits), _ptr(tokens), C.c_int32(logits.shape[0]), C.c_float(temperature),
-                                        C.c_int32(top_k), _ptr(logprob_out), _ptr(entropy_out), _ptr(top_out),
-                                        _ptr(top_logprob_out), _stream()))
+    _check(lib().petals_client_logprobs(client, _at(logits), _at(tokens), logits.shape[0], temperature, top_k, _at(logprob_out),
+                                        _at(entropy_out), _at(top_out), _at(top_logprob_out), _raw_stream()))
 
 
 def petals_client_distill(client, logits, teacher_tokens, teacher_logits, temperature, loss_grad, loss_out, grad_logits_out):
-    _check(lib().petals_client_distill(client, _ptr(logits), C.c_int32(logits.shape[0]), _ptr(teacher_tokens),
-                                       _ptr(teacher_logits), C.c_int32(teacher_tokens.shape[1]), C.c_float(temperature),
-                                       _ptr(loss_grad), _ptr(loss_out), _ptr(grad_logits_out), _stream()))
+    _check(lib().petals_client_distill(client, _at(logits), logits.shape[0], _at(teacher_tokens), _at(teacher_logits),
+                                       teacher_tokens.shape[1], temperature, _at(loss_grad), _at(loss_out),
+                                       _at(grad_logits_out), _raw_stream()))
 
 
 def petals_client_lm_head_backward_bytes(cfg, M):
     n = C.c_size_t()
-    _check(lib().petals_client_lm_head_backward_bytes(C.byref(cfg), C.c_int32(M), C.byref(n)))
+    _check(lib().petals_client_lm_head_backward_bytes(C.byref(cfg), M, C.byref(n)))
     return n.value
 
 
 def petals_client_lm_head_backward(client, store, hidden_in, grad_logits, grad_hidden_out):
-    _check(lib().petals_client_lm_head_backward(client, _ptr(store), _ptr(hidden_in), _ptr(grad_logits),
-                                                C.c_int32(hidden_in.shape[0]), _ptr(grad_hidden_out), _stream()))
+    _check(lib().petals_client_lm_head_backward(client, _at(store), _at(hidden_in), _at(grad_logits), hidden_in.shape[0],
+                                                _at(grad_hidden_out), _raw_stream()))
 
 
 def petals_client_embed_backward(client, token_ids, grad_hidden, tokens_out, grads_out, count_out):
-    _check(lib().petals_client_embed_backward(client, _ptr(token_ids), _ptr(grad_hidden), C.c_int32(token_ids.numel()),
-                                              _ptr(tokens_out), _ptr(grads_out), _ptr(count_out), _stream()))
+    _check(lib().petals_client_embed_backward(client, _at(token_ids), _at(grad_hidden), token_ids.numel(), _at(tokens_out),
+                                              _at(grads_out), _at(count_out), _raw_stream()))
 
 
 class Client:
@@ -544,9 +559,9 @@ class Client:
         petals_client_sample(self.handle, logits, temperature, top_k, uniforms, nxt)
         return nxt
 
-    def _need(self, name, t, dtype, shape):
+    def _need(self, name, t, dtype, *shape):
         """A tensor as the calls below take it: on the client's device, contiguous, of this type and shape."""
-        if not isinstance(t, torch.Tensor) or t.device != self.device or t.dtype != dtype or tuple(t.shape) != tuple(shape) \
+        if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != shape or t.device != self.device \
                 or not t.is_contiguous():
             raise ValueError("%s must be a contiguous %s tensor %s on %s" % (name, dtype, list(shape), self.device))
         return t
@@ -556,22 +571,28 @@ class Client:
             raise ValueError("%s must be a tensor of rows" % name)
         return t.shape[0]
 
+    def _run(self, call, *args):
+        """The call on the client's device and that device's current stream."""
+        if torch.cuda.current_device() == self.device.index:
+            return call(self.handle, *args)
+        with torch.cuda.device(self.device):
+            return call(self.handle, *args)
+
     def logprobs(self, logits, tokens=None, temperature=1.0, top_k=0):
         """Log probabilities fp32 [M] of int32 tokens [M] under softmax(logits / temperature) of fp32 logits [M, V] (0 for a token
         outside the vocabulary), entropies fp32 [M], and the top_k most likely tokens int32 [M, top_k] with their log
         probabilities fp32 [M, top_k]; None for what was not asked for."""
         M = self._rows("logits", logits)
-        self._need("logits", logits, torch.float32, (M, self.vocab))
+        self._need("logits", logits, torch.float32, M, self.vocab)
         if tokens is not None:
-            self._need("tokens", tokens, torch.int32, (M,))
+            self._need("tokens", tokens, torch.int32, M)
         if not 0 <= top_k <= self.vocab:
             raise ValueError("top_k must be between 0 and the vocabulary")
         new = lambda dtype, *shape: torch.empty(shape, dtype=dtype, device=self.device)   # noqa: E731
         logprob = new(torch.float32, M) if tokens is not None else None
         entropy = new(torch.float32, M)
         top, top_logprob = (new(torch.int32, M, top_k), new(torch.float32, M, top_k)) if top_k else (None, None)
-        with torch.cuda.device(self.device):
-            petals_client_logprobs(self.handle, logits, tokens, temperature, top_k, logprob, entropy, top, top_logprob)
+        self._run(petals_client_logprobs, logits, tokens, temperature, top_k, logprob, entropy, top, top_logprob)
         return logprob, entropy, top, top_logprob
 
     def distill(self, logits, teacher_tokens, teacher_logits, temperature=1.0, loss_grad=None, want_grad=True, grad_out=None):
@@ -579,33 +600,31 @@ class Client:
         [M, K]), and the gradient fp32 [M, V] of sum(loss_grad * loss) (loss_grad fp32 [M]; None: ones), which may go into the
         logits' own memory (grad_out=logits).  One teacher token per row: cross-entropy."""
         M, K = self._rows("logits", logits), self._rows("teacher_tokens", teacher_tokens) and teacher_tokens.shape[1]
-        self._need("logits", logits, torch.float32, (M, self.vocab))
-        self._need("teacher_tokens", teacher_tokens, torch.int32, (M, K))
-        self._need("teacher_logits", teacher_logits, torch.float32, (M, K))
+        self._need("logits", logits, torch.float32, M, self.vocab)
+        self._need("teacher_tokens", teacher_tokens, torch.int32, M, K)
+        self._need("teacher_logits", teacher_logits, torch.float32, M, K)
         if loss_grad is not None:
-            self._need("loss_grad", loss_grad, torch.float32, (M,))
+            self._need("loss_grad", loss_grad, torch.float32, M)
         if grad_out is not None:
-            self._need("grad_out", grad_out, torch.float32, (M, self.vocab))
+            self._need("grad_out", grad_out, torch.float32, M, self.vocab)
         loss = torch.empty(M, dtype=torch.float32, device=self.device)
         grad = grad_out if grad_out is not None else torch.empty_like(logits) if want_grad else None
-        with torch.cuda.device(self.device):
-            petals_client_distill(self.handle, logits, teacher_tokens, teacher_logits, temperature, loss_grad, loss, grad)
+        self._run(petals_client_distill, logits, teacher_tokens, teacher_logits, temperature, loss_grad, loss, grad)
         return loss, grad
 
     def lm_head_backward(self, hidden, grad_logits, store=None, out=None):
         """Gradient fp16 [M, H] of lm_head's hidden states fp16 [M, H] from that of its logits, fp32 [M, V].  store: a uint8
         tensor of at least petals_client_lm_head_backward_bytes to reuse between calls."""
         M = self._rows("hidden", hidden)
-        self._need("hidden", hidden, torch.float16, (M, self.hidden))
-        self._need("grad_logits", grad_logits, torch.float32, (M, self.vocab))
+        self._need("hidden", hidden, torch.float16, M, self.hidden)
+        self._need("grad_logits", grad_logits, torch.float32, M, self.vocab)
         need = petals_client_lm_head_backward_bytes(self.cfg, M)
         if store is None:
             store = torch.empty(need, dtype=torch.uint8, device=self.device)
         if store.device != self.device or store.dtype != torch.uint8 or not store.is_contiguous() or store.numel() < need:
             raise ValueError("store must be a uint8 tensor of at least %d bytes on %s" % (need, self.device))
-        out = torch.empty_like(hidden) if out is None else self._need("out", out, torch.float16, (M, self.hidden))
-        with torch.cuda.device(self.device):
-            petals_client_lm_head_backward(self.handle, store, hidden, grad_logits, out)
+        out = torch.empty_like(hidden) if out is None else self._need("out", out, torch.float16, M, self.hidden)
+        self._run(petals_client_lm_head_backward, store, hidden, grad_logits, out)
         return out
 
     def embed_backward(self, token_ids, grad_hidden, out=None):
@@ -613,17 +632,16 @@ class Client:
         order, their rows' gradients fp32 [M, H] and their number int32 [1]; entries from that number on are left as they
         were (out: the three tensors to use)."""
         M = self._rows("grad_hidden", grad_hidden)
-        self._need("token_ids", token_ids, torch.int32, (M,))
-        self._need("grad_hidden", grad_hidden, torch.float16, (M, self.hidden))
+        self._need("token_ids", token_ids, torch.int32, M)
+        self._need("grad_hidden", grad_hidden, torch.float16, M, self.hidden)
         if out is None:
             out = (torch.empty(M, dtype=torch.int32, device=self.device),
                    torch.empty((M, self.hidden), dtype=torch.float32, device=self.device),
                    torch.empty(1, dtype=torch.int32, device=self.device))
-        self._need("out[0]", out[0], torch.int32, (M,))
-        self._need("out[1]", out[1], torch.float32, (M, self.hidden))
-        self._need("out[2]", out[2], torch.int32, (1,))
-        with torch.cuda.device(self.device):
-            petals_client_embed_backward(self.handle, token_ids, grad_hidden, *out)
+        self._need("out[0]", out[0], torch.int32, M)
+        self._need("out[1]", out[1], torch.float32, M, self.hidden)
+        self._need("out[2]", out[2], torch.int32, 1)
+        self._run(petals_client_embed_backward, token_ids, grad_hidden, *out)
         return out
 
     def close(self):

@@ -9,15 +9,6 @@
 #include "host_util.h"
 #include "ln_backward.h"
 
-#ifndef DGB
-#define DGB 96
-#endif
-#ifndef PREF
-#define PREF 1
-#endif
-#ifndef RG
-#define RG 1024
-#endif
 namespace {
 
 // ------------------------------------------------------------------------------------ a row's softmax statistics
@@ -83,25 +74,26 @@ __device__ __forceinline__ float accumulate(RowStat &s, const float (&l)[N], flo
 constexpr int ROW_NT = 256, ROW_NW = ROW_NT / 64;
 constexpr int ROW_PER = 16;                         // logits of a thread per step
 constexpr int WAVE_STEP = 64 * ROW_PER, ROW_STEP = ROW_NW * WAVE_STEP;
-constexpr int ROW_GROUPS = RG;                    // workgroups that keep the memory busy: 4 per compute unit
+constexpr int LOGPROBS_GROUPS = 1024, DISTILL_GROUPS = 2048;
 typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));     // rows of an odd vocabulary begin anywhere
 
 // A call of few rows shares each row out over workgroups, a whole number of steps to each.
 struct RowSplit {
     int splits, range;
 };
-RowSplit row_split(int M, int V, int most) {
-    const int steps = (V + ROW_STEP - 1) / ROW_STEP, want = max(1, min(min(steps, most), (ROW_GROUPS + M - 1) / M)), per = (steps + want - 1) / want;
+RowSplit row_split(int M, int V, int groups, int most) {
+    const int steps = (V + ROW_STEP - 1) / ROW_STEP, want = max(1, min(min(steps, most), (groups + M - 1) / M)), per = (steps + want - 1) / want;
     return RowSplit{(steps + per - 1) / per, per * ROW_STEP};
 }
 
 // logit 4 q + e of a thread's step is column v0 + 256 q + 4 lane + e, v0 = the wave's first; what lies behind the row is -infinity
+template <bool LAST>
 __device__ __forceinline__ void load_logits(const float *row, int v0, int end, float (&l)[ROW_PER]) {
     const int first = v0 + 4 * (threadIdx.x & 63);
     if (v0 + WAVE_STEP <= end) {
 #pragma unroll
         for (int q = 0; q < ROW_PER / 4; q++) {
-            const v4f f = *(const v4f_any *)(row + first + 256 * q);
+            const v4f f = LAST ? __builtin_nontemporal_load((const v4f_any *)(row + first + 256 * q)) : *(const v4f_any *)(row + first + 256 * q);
 #pragma unroll
             for (int e = 0; e < 4; e++) l[4 * q + e] = f[e];
         }
@@ -113,26 +105,15 @@ __device__ __forceinline__ void load_logits(const float *row, int v0, int end, f
         }
     }
 }
-// the steps of this wave in [begin, end), the next one's logits on their way while one is worked on: step(first column, logits)
-template <typename F>
+// the steps of this wave in [begin, end): step(first column, logits).  (The other waves of the compute unit cover the wait for
+// a step's logits: with the next step's asked for ahead, in 16 more registers, 1024 x 250880 took 223 instead of 218 us.)
+template <bool LAST = false, typename F>
 __device__ __forceinline__ void walk_row(const float *row, int begin, int end, F step) {
-#if PREF
-    float l[ROW_PER], ahead[ROW_PER];
-    int v = begin + (threadIdx.x >> 6) * WAVE_STEP;
-    if (v < end) load_logits(row, v, end, l);
-    for (; v < end; v += ROW_STEP) {
-        if (v + ROW_STEP < end) load_logits(row, v + ROW_STEP, end, ahead);
-        step(v, l);
-#pragma unroll
-        for (int i = 0; i < ROW_PER; i++) l[i] = ahead[i];
-    }
-#else
     for (int v = begin + (threadIdx.x >> 6) * WAVE_STEP; v < end; v += ROW_STEP) {
         float l[ROW_PER];
-        load_logits(row, v, end, l);
+        load_logits<LAST>(row, v, end, l);
         step(v, l);
     }
-#endif
 }
 
 // ------------------------------------------------------------------------------------ the largest logits of a row
@@ -148,12 +129,22 @@ __device__ __forceinline__ float key_value(uint64_t key) {
     const uint32_t u = (uint32_t)(key >> 32);
     return __uint_as_float((u & 0x80000000u) ? u & 0x7fffffffu : ~u);
 }
-__device__ __forceinline__ int key_index(uint64_t key) { return (int)~(uint32_t)key; }
+// (in range also where a row of NaN has left a place of the list empty)
+__device__ __forceinline__ int key_index(uint64_t key) { return key ? (int)~(uint32_t)key : 0; }
 __device__ __forceinline__ uint64_t read_lane(uint64_t v, int lane) {
     return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
 }
 struct TopList {
-    uint64_t key = 0, last = 0;         // this lane's key; the one at place top_k - 1
+    uint64_t key = 0, floor = 0, last = 0;         // this lane's key; what is no larger than these two does not come in
+    // most: every lane's largest logit of its first step.  The top_k-th largest of the 64 lanes' is a bound that at least top_k
+    // logits of the step reach, so that a few more than top_k come in instead of top_k (1 + log(1024 / top_k)).
+    __device__ __forceinline__ void start(float most, int top_k) {
+        int above = 0;
+#pragma unroll
+        for (int i = 0; i < 64; i++) above += __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(most), i)) > most;
+        floor = ((uint64_t)order_key(-wave_max(above < top_k ? -most : -INFINITY)) << 32) - 1;
+        last = floor;
+    }
     __device__ __forceinline__ void offer(uint64_t k, int top_k) {        // one key per lane, 0: none
         const int lane = threadIdx.x & 63;
         unsigned long long who = __ballot(k > last);
@@ -163,7 +154,7 @@ struct TopList {
             if (lane == from) k = 0;
             const uint64_t prev = (uint64_t)dpp_move<0x138, 0xf>(0u, (uint32_t)(key >> 32)) << 32 | dpp_move<0x138, 0xf>(0u, (uint32_t)key);   // wave_shr 1
             if (key < nk) key = lane == 0 || prev > nk ? nk : prev;
-            last = read_lane(key, top_k - 1);
+            last = max(floor, read_lane(key, top_k - 1));
             who = __ballot(k > last);
         }
     }
@@ -193,13 +184,12 @@ __device__ __forceinline__ void logprobs_store(const LogprobsOut &o, int t, int 
     }
 }
 // the waves' lists become the first wave's
-template <int NW>
-__device__ __forceinline__ void join_lists(TopList &list, uint64_t (*lists)[64], int top_k) {
+__device__ __forceinline__ void join_lists(TopList &list, uint64_t (*lists)[64], int top_k, int nw) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     lists[wave][lane] = list.key;
     __syncthreads();
     if (wave == 0)
-        for (int w = 1; w < NW; w++) list.offer(lists[w][lane], top_k);
+        for (int w = 1; w < nw; w++) list.offer(lists[w][lane], top_k);
 }
 
 // workgroup (split, row): the split's part of the row, and with one split the results
@@ -213,7 +203,8 @@ __global__ void __launch_bounds__(ROW_NT) k_logprobs(LogprobsOut o, int V, int r
     TopList list;
     walk_row(o.logits + (size_t)t * V, begin, end, [&](int v0, const float (&l)[ROW_PER]) {
         const float most = accumulate<ROW_PER, true>(s, l, c, invT);
-        if (top_k && __ballot(!(most < key_value(list.last)))) {
+        if (top_k && v0 < begin + ROW_STEP) list.start(most, top_k);
+        if (top_k && __ballot(!(most < key_value(list.last + 1)))) {
 #pragma unroll
             for (int i = 0; i < ROW_PER; i++) {
                 const int v = v0 + 4 * lane + 256 * (i >> 2) + (i & 3);
@@ -222,7 +213,7 @@ __global__ void __launch_bounds__(ROW_NT) k_logprobs(LogprobsOut o, int V, int r
         }
     });
     s = block_merge<ROW_NW>(s, invT, sm);
-    if (top_k) join_lists<ROW_NW>(list, lists, top_k);
+    if (top_k) join_lists(list, lists, top_k, ROW_NW);
     if (gridDim.x == 1) {
         logprobs_store(o, t, V, invT, top_k, s, list);
         return;
@@ -245,7 +236,7 @@ __global__ void __launch_bounds__(JOIN_NT) k_logprobs_join(LogprobsOut o, int V,
     const uint64_t *keys = tops + (size_t)t * n;
     for (int i = threadIdx.x; i < (n + 63) / 64 * 64; i += JOIN_NT) list.offer(i < n ? keys[i] : 0, top_k);
     s = block_merge<JOIN_NW>(s, invT, sm);
-    if (top_k) join_lists<JOIN_NW>(list, lists, top_k);
+    if (top_k) join_lists(list, lists, top_k, min(JOIN_NW, (n + 63) / 64));
     logprobs_store(o, t, V, invT, top_k, s, list);
 }
 
@@ -406,7 +397,7 @@ __device__ __forceinline__ void distill_grad(const DistillIn &d, int t, const Di
         for (int v0 = begin + (threadIdx.x >> 6) * WAVE_STEP; v0 < end; v0 += ROW_STEP) store(v0, g);
         return;
     }
-    walk_row(row, begin, end, [&](int v0, const float (&l)[ROW_PER]) {
+    walk_row<true>(row, begin, end, [&](int v0, const float (&l)[ROW_PER]) {
         float g[ROW_PER];
 #pragma unroll
         for (int i = 0; i < ROW_PER; i++) g[i] = f * __builtin_amdgcn_exp2f((l[i] - m) * c);
@@ -426,10 +417,14 @@ __global__ void __launch_bounds__(ROW_NT) k_distill(DistillIn d, int first2, int
     __shared__ float sf[ROW_NW];
     __shared__ int s_id[PETALS_DISTILL_TOP_MAX];
     __shared__ double s_p[PETALS_DISTILL_TOP_MAX];
-    if ((int)blockIdx.y < n2) {
-        distill_grad(d, first2 + (int)blockIdx.y, parts, rows, s_id, s_p);
+    // the two kinds take turns, as far as there are both
+    const int y = blockIdx.y, n1 = (int)gridDim.y - n2, both = 2 * min(n1, n2);
+    const bool second = y < both ? !(y & 1) : both ? n2 > n1 : y < n2;
+    const int i = y < both ? y >> 1 : both ? y - both / 2 : second ? y : y - n2;
+    if (second) {
+        distill_grad(d, first2 + i, parts, rows, s_id, s_p);
     } else {
-        const int t = first1 + (int)blockIdx.y - n2;
+        const int t = first1 + i;
         distill_stats(d, t, parts + (size_t)t * gridDim.x + blockIdx.x, rows + t, sm, sd, sf);
     }
 }
@@ -445,48 +440,84 @@ struct Place {
     int position, before, count;      // the position; how many earlier ones have its token, and how many in all
 };
 constexpr int RUN_PIECE = 32;         // positions that one workgroup sums; a longer list goes in pieces of 32 to 63
+constexpr int PLACE_ROWS = 16;        // positions of a workgroup, compared with all of the call's by 64 groups of 16 threads
 
-__global__ void __launch_bounds__(1024) k_token_places(const int32_t *__restrict__ ids, int M, int V, Place *__restrict__ places) {
-    __shared__ int tile[1024];
-    __shared__ int less[16][64], same[16][64], all[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = blockIdx.x * 64 + lane;
-    const int own = i < M ? min(max(ids[i], 0), V - 1) : 0;
+// first: a byte per place, 1 where a token begins
+__global__ void __launch_bounds__(1024) k_token_places(const int32_t *__restrict__ ids, int M, int V, Place *__restrict__ places,
+                                                       uint8_t *__restrict__ first) {
+    __shared__ __align__(16) int tile[1024];
+    __shared__ int sums[3][64][PLACE_ROWS];
+    const int g = threadIdx.x / PLACE_ROWS, r = threadIdx.x % PLACE_ROWS, i0 = blockIdx.x * PLACE_ROWS, i = i0 + r;
+    const int own = min(max(ids[min(i, M - 1)], 0), V - 1);
     int n_less = 0, n_before = 0, n_all = 0;
     for (int j0 = 0; j0 < M; j0 += 1024) {
         const int j = j0 + threadIdx.x;
         __syncthreads();
-        tile[threadIdx.x] = j < M ? min(max(ids[j], 0), V - 1) : 0x7fffffff;
+        tile[threadIdx.x] = j < M ? min(max(ids[j], 0), V - 1) : 0x7fffffff;       // (no token)
         __syncthreads();
-        for (int u = wave * 64; u < wave * 64 + 64; u++) {
-            const int o = tile[u];
-            n_less += o < own;
-            n_all += o == own;
-            n_before += o == own && j0 + u < i;
+        const v4i *mine = (const v4i *)tile + g * 4;
+        if (j0 + 1024 <= i0 || j0 >= i0 + PLACE_ROWS) {                            // all of them before, or behind, these positions
+            const int border = own + (j0 < i0);
+            int n = 0;
+#pragma unroll
+            for (int q = 0; q < 4; q++) {
+                const v4i o = mine[q];
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    n_less += o[e] < border;
+                    n += o[e] == own;
+                }
+            }
+            n_all += n;
+            if (j0 < i0) {                                                          // (n_less has them already)
+                n_before += n;
+                n_less -= n;
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; q++) {
+                const v4i o = mine[q];
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    n_less += o[e] < own;
+                    n_all += o[e] == own;
+                    n_before += o[e] == own && j0 + g * 16 + q * 4 + e < i;
+                }
+            }
         }
     }
-    less[wave][lane] = n_less;
-    same[wave][lane] = n_before;
-    all[wave][lane] = n_all;
+    sums[0][g][r] = n_less;
+    sums[1][g][r] = n_before;
+    sums[2][g][r] = n_all;
     __syncthreads();
-    if (wave == 0 && i < M) {
-        n_less = n_before = n_all = 0;
-        for (int w = 0; w < 16; w++) {
-            n_less += less[w][lane];
-            n_before += same[w][lane];
-            n_all += all[w][lane];
+    if (threadIdx.x < 64) {                                                         // 4 lanes share a position's 64 sums
+        const int p = threadIdx.x >> 2, part = threadIdx.x & 3;
+        uint32_t n[3];
+#pragma unroll
+        for (int c = 0; c < 3; c++) {
+            n[c] = 0;
+#pragma unroll
+            for (int u = 0; u < 16; u++) n[c] += sums[c][part * 16 + u][p];
+            n[c] = group_reduce<4>(n[c], [](uint32_t a, uint32_t b) { return a + b; });
         }
-        places[n_less + n_before] = Place{i, n_before, n_all};
+        if (part == 0 && i0 + p < M) {
+            places[n[0] + n[1]] = Place{i0 + p, (int)n[1], (int)n[2]};
+            first[n[0] + n[1]] = n[1] == 0;
+        }
     }
 }
 
 // How many pieces a list of n positions has, each of RUN_PIECE but the last, which takes what is left over as well
 __device__ __forceinline__ int run_pieces(int n) { return max(1, n / RUN_PIECE); }
 
-// number of different tokens before place p (over the workgroup)
+// number of different tokens before place p (over the workgroup); first is padded to 8 bytes
 template <int NT>
-__device__ __forceinline__ int tokens_before(const Place *__restrict__ places, int p, int *sm) {
+__device__ __forceinline__ int tokens_before(const uint8_t *__restrict__ first, int p, int *sm) {
     int n = 0;
-    for (int q = threadIdx.x; q < p; q += NT) n += places[q].before == 0;
+    for (int q = threadIdx.x * 8; q < p; q += NT * 8) {
+        const uint64_t w = *(const uint64_t *)(first + q);
+        n += __popcll(p - q >= 8 ? w : w & ((1ull << (8 * (p - q))) - 1));
+    }
     n = (int)wave_sum((float)n);                                     // at most 2^24 of them
     if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = n;
     __syncthreads();
@@ -497,96 +528,85 @@ __device__ __forceinline__ int tokens_before(const Place *__restrict__ places, i
     return n;
 }
 
+// acc += rows 0 .. n - 1 in order, row(r) the address of row r; eight of them on their way at once
+template <int NT, int PER, typename T, typename F>
+__device__ __forceinline__ void add_rows(float (&acc)[PER][8], int n, int H, F row) {
+    constexpr int AHEAD = 8;
+    typedef T v8 __attribute__((ext_vector_type(8), aligned(2)));
+    for (int r0 = 0; r0 < n; r0 += AHEAD) {
+        const T *from[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; u++) from[u] = row(min(r0 + u, n - 1));
+#pragma unroll
+        for (int i = 0; i < PER; i++) {
+            const int k = (threadIdx.x + i * NT) * 8;
+            if (k >= H) continue;
+            v8 f[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; u++) f[u] = *(const v8 *)(from[u] + k);
+#pragma unroll
+            for (int u = 0; u < AHEAD; u++)
+                if (r0 + u < n) {
+#pragma unroll
+                    for (int e = 0; e < 8; e++) acc[i][e] += (float)f[u][e];
+                }
+        }
+    }
+}
+
 // one workgroup per place: a place at which a piece of a token's list begins has work
 template <int NT, int PER>
 __global__ void __launch_bounds__(NT) k_embed_backward(const int32_t *__restrict__ ids, const __half *__restrict__ grad, int M, int V,
                                                        int H, const __half *__restrict__ E, const __half *__restrict__ g, float eps,
-                                                       const Place *__restrict__ places, float *__restrict__ parts,
-                                                       int32_t *__restrict__ tokens_out, float *__restrict__ grads_out,
-                                                       int32_t *__restrict__ count_out) {
+                                                       const Place *__restrict__ places, const uint8_t *__restrict__ first,
+                                                       float *__restrict__ parts, int32_t *__restrict__ tokens_out,
+                                                       float *__restrict__ grads_out, int32_t *__restrict__ count_out) {
     __shared__ double sd[NT / 64][2];
     __shared__ int si[NT / 64];
     const int p = blockIdx.x;
     const Place pl = places[p];
     const int piece = pl.before / RUN_PIECE, pieces = run_pieces(pl.count);
-    if (pl.before % RUN_PIECE || piece >= pieces) {
-        if (p == M - 1) {                                            // not the first of its token: the count is still to be told
-            const int n = tokens_before<NT>(places, M, si);
-            if (threadIdx.x == 0) *count_out = n;
-        }
-        return;
+    if (p == M - 1) {
+        const int n = tokens_before<NT>(first, M, si);
+        if (threadIdx.x == 0) *count_out = n;
     }
+    if (pl.before % RUN_PIECE || piece >= pieces) return;
     const int n = piece == pieces - 1 ? pl.count - pl.before : RUN_PIECE;
-    float acc[PER][8];
-#pragma unroll
-    for (int i = 0; i < PER; i++)
-#pragma unroll
-        for (int e = 0; e < 8; e++) acc[i][e] = 0.0f;
-    for (int r = 0; r < n; r++) {
-        const __half *row = grad + (size_t)places[p + r].position * H;
-#pragma unroll
-        for (int i = 0; i < PER; i++) {
-            const int k = (threadIdx.x + i * NT) * 8;
-            if (k < H) {
-                const v8h f = *(const v8h_any *)(row + k);
-#pragma unroll
-                for (int e = 0; e < 8; e++) acc[i][e] += (float)f[e];
-            }
-        }
-    }
+    float acc[PER][8] = {};
+    add_rows<NT, PER, _Float16>(acc, n, H, [&](int r) { return (const _Float16 *)grad + (size_t)places[p + r].position * H; });
     if (pieces > 1) {                                                // pieces begin at least RUN_PIECE places apart
         ln_store<NT, PER>(acc, parts + (size_t)(p / RUN_PIECE) * H, H);
-    } else {
-        const int u = tokens_before<NT>(places, p, si), token = min(max(ids[pl.position], 0), V - 1);
-        ln_backward<NT, PER>(acc, E + (size_t)token * H, g, H, eps, sd);
-        ln_store<NT, PER>(acc, grads_out + (size_t)u * H, H);
-        if (threadIdx.x == 0) tokens_out[u] = token;
+        return;
     }
-    if (p == M - 1) {
-        const int all = tokens_before<NT>(places, M, si);
-        if (threadIdx.x == 0) *count_out = all;
-    }
+    const int u = tokens_before<NT>(first, p, si), token = min(max(ids[pl.position], 0), V - 1);
+    ln_backward<NT, PER>(acc, E + (size_t)token * H, g, H, eps, sd);
+    ln_store<NT, PER>(acc, grads_out + (size_t)u * H, H);
+    if (threadIdx.x == 0) tokens_out[u] = token;
 }
 
 // the lists of several pieces: workgroup b looks for one that begins at places b * RUN_PIECE ..
 template <int NT, int PER>
 __global__ void __launch_bounds__(NT) k_embed_backward_join(const int32_t *__restrict__ ids, int M, int V, int H,
                                                             const __half *__restrict__ E, const __half *__restrict__ g, float eps,
-                                                            const Place *__restrict__ places, const float *__restrict__ parts,
-                                                            int32_t *__restrict__ tokens_out, float *__restrict__ grads_out) {
+                                                            const Place *__restrict__ places, const uint8_t *__restrict__ first,
+                                                            const float *__restrict__ parts, int32_t *__restrict__ tokens_out,
+                                                            float *__restrict__ grads_out) {
     __shared__ double sd[NT / 64][2];
     __shared__ int si[NT / 64];
-    __shared__ int s_at;
-    if (threadIdx.x == 0) s_at = -1;
-    __syncthreads();
-    const int q = blockIdx.x * RUN_PIECE + threadIdx.x;
-    if (threadIdx.x < RUN_PIECE && q < M && places[q].before == 0 && run_pieces(places[q].count) > 1) s_at = q;      // at most one
-    __syncthreads();
-    const int p = s_at;
-    if (p < 0) return;
+    const int lane = threadIdx.x & 63, q = blockIdx.x * RUN_PIECE + lane;
+    bool begins = false;
+    if (lane < RUN_PIECE && q < M) {
+        const Place pl = places[q];
+        begins = pl.before == 0 && run_pieces(pl.count) > 1;         // at most one does
+    }
+    const unsigned long long who = __ballot(begins);                 // (every wave for itself)
+    if (!who) return;
+    const int p = blockIdx.x * RUN_PIECE + __builtin_ctzll(who);
     const Place pl = places[p];
     const int pieces = run_pieces(pl.count), token = min(max(ids[pl.position], 0), V - 1);
-    float acc[PER][8];
-#pragma unroll
-    for (int i = 0; i < PER; i++)
-#pragma unroll
-        for (int e = 0; e < 8; e++) acc[i][e] = 0.0f;
-    for (int r = 0; r < pieces; r++) {
-        const float *row = parts + (size_t)((p + r * RUN_PIECE) / RUN_PIECE) * H;
-#pragma unroll
-        for (int i = 0; i < PER; i++) {
-            const int k = (threadIdx.x + i * NT) * 8;
-            if (k < H) {
-#pragma unroll
-                for (int h = 0; h < 2; h++) {
-                    const v4f f = *(const v4f *)(row + k + 4 * h);
-#pragma unroll
-                    for (int e = 0; e < 4; e++) acc[i][4 * h + e] += f[e];
-                }
-            }
-        }
-    }
-    const int u = tokens_before<NT>(places, p, si);
+    float acc[PER][8] = {};
+    add_rows<NT, PER, float>(acc, pieces, H, [&](int r) { return parts + (size_t)(p / RUN_PIECE + r) * H; });
+    const int u = tokens_before<NT>(first, p, si);
     ln_backward<NT, PER>(acc, E + (size_t)token * H, g, H, eps, sd);
     ln_store<NT, PER>(acc, grads_out + (size_t)u * H, H);
     if (threadIdx.x == 0) tokens_out[u] = token;
@@ -594,10 +614,11 @@ __global__ void __launch_bounds__(NT) k_embed_backward_join(const int32_t *__res
 
 template <int NT, int PER>
 void embed_backward(const int32_t *ids, const __half *grad, int M, int V, int H, const __half *E, const __half *g, float eps,
-                    const Place *places, float *parts, int32_t *tokens_out, float *grads_out, int32_t *count_out, hipStream_t st) {
-    k_embed_backward<NT, PER><<<M, NT, 0, st>>>(ids, grad, M, V, H, E, g, eps, places, parts, tokens_out, grads_out, count_out);
+                    const Place *places, const uint8_t *first, float *parts, int32_t *tokens_out, float *grads_out, int32_t *count_out,
+                    hipStream_t st) {
+    k_embed_backward<NT, PER><<<M, NT, 0, st>>>(ids, grad, M, V, H, E, g, eps, places, first, parts, tokens_out, grads_out, count_out);
     if (M >= 2 * RUN_PIECE)
-        k_embed_backward_join<NT, PER><<<(M + RUN_PIECE - 1) / RUN_PIECE, NT, 0, st>>>(ids, M, V, H, E, g, eps, places, parts, tokens_out, grads_out);
+        k_embed_backward_join<NT, PER><<<(M + RUN_PIECE - 1) / RUN_PIECE, NT, 0, st>>>(ids, M, V, H, E, g, eps, places, first, parts, tokens_out, grads_out);
 }
 
 int check_call(const petals_client_config &cfg, int32_t M) {
@@ -606,7 +627,7 @@ int check_call(const petals_client_config &cfg, int32_t M) {
     return PETALS_OK;
 }
 constexpr int MAX_GRID_ROWS = 1 << 14;      // rows of a group (two groups share the grid's second dimension)
-constexpr size_t DISTILL_GROUP_BYTES = (size_t)DGB << 20;
+constexpr size_t DISTILL_GROUP = (size_t)128 << 20, DISTILL_ONE_GROUP = (size_t)192 << 20;
 bool usable_temperature(float t) { return t > 0.0f && t < INFINITY && 1.0f / t < INFINITY; }
 
 }  // namespace
@@ -632,7 +653,7 @@ int petals_client_logprobs(petals_client *client, const float *logits, const int
     const double invT = 1.0 / (double)temperature;
     // per row and split in the workspace: its statistics and its list
     const size_t per = sizeof(RowStat) + sizeof(uint64_t) * top_k;
-    const RowSplit sp = row_split(M, V, (int)min((size_t)1 << 20, c.scratch_bytes / ((size_t)M * per)));
+    const RowSplit sp = row_split(M, V, LOGPROBS_GROUPS, (int)min((size_t)1 << 20, c.scratch_bytes / ((size_t)M * per)));
     RowStat *stats = (RowStat *)c.scratch;
     uint64_t *tops = (uint64_t *)(stats + (size_t)M * sp.splits);
     for (int t0 = 0; t0 < M; t0 += MAX_GRID_ROWS) {
@@ -664,9 +685,11 @@ int petals_client_distill(petals_client *client, const float *logits, int32_t M,
     const int V = c.cfg->vocab;
     DistillRow *rows = (DistillRow *)c.scratch;
     DistillPart *parts = (DistillPart *)(rows + M);
-    const int group = grad_logits_out ? (int)max((size_t)1, min((size_t)MAX_GRID_ROWS, DISTILL_GROUP_BYTES / ((size_t)V * sizeof(float)))) : MAX_GRID_ROWS;
+    const size_t row_bytes = (size_t)V * sizeof(float);
+    const int group = !grad_logits_out || row_bytes * M <= DISTILL_ONE_GROUP ? MAX_GRID_ROWS
+                                       : (int)max((size_t)1, min((size_t)MAX_GRID_ROWS, DISTILL_GROUP / row_bytes));
     const size_t room = (c.scratch_bytes - sizeof(DistillRow) * M) / ((size_t)M * sizeof(DistillPart));
-    const RowSplit sp = row_split(min(M, group), V, (int)min((size_t)1 << 20, room));
+    const RowSplit sp = row_split(min(M, group), V, DISTILL_GROUPS, (int)min((size_t)1 << 20, room));
     const DistillIn d{logits, teacher_tokens, teacher_logits, loss_grad, loss_out, grad_logits_out, V, K, sp.range, (double)temperature, 1.0 / (double)temperature};
     for (int t0 = 0, n2 = 0; t0 < M || n2; t0 += group) {
         const int n1 = max(0, min(group, M - t0));
@@ -684,17 +707,18 @@ int petals_client_embed_backward(petals_client *client, const int32_t *token_ids
     if (int rc = check_call(*c.cfg, M)) return rc;
     if (token_ids == tokens_out) return ps_fail(PETALS_ERR_INVALID_ARG, "token_ids and tokens_out alias");
     const int V = c.cfg->vocab, H = c.cfg->hidden;
-    // M places of 12 bytes, then a row of partial sums for every RUN_PIECE places: 12 M + (M / 32 + 1) 4 H bytes
+    // M places of 12 bytes and their flags, then a row of partial sums for every RUN_PIECE places: some 13 M + (M / 32 + 1) 4 H bytes
     Place *places = (Place *)c.scratch;
-    float *parts = (float *)(c.scratch + ((size_t)M * sizeof(Place) + 255) / 256 * 256);
+    uint8_t *first = (uint8_t *)(places + (M + 1) / 2 * 2);
+    float *parts = (float *)(c.scratch + ((size_t)(first - c.scratch) + M + 255) / 256 * 256);
     hipStream_t st = (hipStream_t)stream;
     const __half *E = (const __half *)c.p->embeddings, *g = (const __half *)c.p->emb_ln_g, *gr = (const __half *)grad_hidden;
     const float eps = c.cfg->ln_eps;
-    k_token_places<<<(M + 63) / 64, 1024, 0, st>>>(token_ids, M, V, places);
-    if (H <= 2048) embed_backward<256, 1>(token_ids, gr, M, V, H, E, g, eps, places, parts, tokens_out, grads_out, count_out, st);
-    else if (H <= 4096) embed_backward<512, 1>(token_ids, gr, M, V, H, E, g, eps, places, parts, tokens_out, grads_out, count_out, st);
-    else if (H <= 8192) embed_backward<1024, 1>(token_ids, gr, M, V, H, E, g, eps, places, parts, tokens_out, grads_out, count_out, st);
-    else embed_backward<1024, 2>(token_ids, gr, M, V, H, E, g, eps, places, parts, tokens_out, grads_out, count_out, st);
+    k_token_places<<<(M + PLACE_ROWS - 1) / PLACE_ROWS, 1024, 0, st>>>(token_ids, M, V, places, first);
+    if (H <= 2048) embed_backward<256, 1>(token_ids, gr, M, V, H, E, g, eps, places, first, parts, tokens_out, grads_out, count_out, st);
+    else if (H <= 4096) embed_backward<512, 1>(token_ids, gr, M, V, H, E, g, eps, places, first, parts, tokens_out, grads_out, count_out, st);
+    else if (H <= 8192) embed_backward<1024, 1>(token_ids, gr, M, V, H, E, g, eps, places, first, parts, tokens_out, grads_out, count_out, st);
+    else embed_backward<1024, 2>(token_ids, gr, M, V, H, E, g, eps, places, first, parts, tokens_out, grads_out, count_out, st);
     HIP_TRY(hipGetLastError());
     return PETALS_OK;
 }
