@@ -493,8 +493,8 @@ def _at(t):
     return None if t is None else t.data_ptr()
 
 
-def _raw_stream():
-    return torch.cuda.current_stream().cuda_stream
+def _raw_stream():      # (torch.cuda.current_stream() makes a Stream object, 3 us; a call of one row takes 12 us on the GPU)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def petals_client_logprobs(client, logits, tokens, temperature, top_k, logprob_out, entropy_out, top_out, top_logprob_out):

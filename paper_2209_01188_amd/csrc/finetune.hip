@@ -9,6 +9,12 @@
 #include "host_util.h"
 #include "ln_backward.h"
 
+#ifndef AH
+#define AH 4
+#endif
+#ifndef EO
+#define EO 1
+#endif
 namespace {
 
 // ------------------------------------------------------------------------------------ a row's softmax statistics
@@ -436,8 +442,8 @@ __global__ void __launch_bounds__(ROW_NT) k_distill(DistillIn d, int first2, int
 //
 // Places in token order by counting: place of position i = number of j with (token_j, j) < (token_i, i).  No order of
 // atomics enters, and a call of a few thousand positions is a few million comparisons.
-struct Place {
-    int position, before, count;      // the position; how many earlier ones have its token, and how many in all
+struct __align__(16) Place {
+    int position, token, before, count;      // a position and its token; how many earlier ones have the same, and how many in all
 };
 constexpr int RUN_PIECE = 32;         // positions that one workgroup sums; a longer list goes in pieces of 32 to 63
 constexpr int PLACE_ROWS = 16;        // positions of a workgroup, compared with all of the call's by 64 groups of 16 threads
@@ -491,7 +497,7 @@ __global__ void __launch_bounds__(1024) k_token_places(const int32_t *__restrict
     sums[2][g][r] = n_all;
     __syncthreads();
     if (threadIdx.x < 64) {                                                         // 4 lanes share a position's 64 sums
-        const int p = threadIdx.x >> 2, part = threadIdx.x & 3;
+        const int p = threadIdx.x >> 2, part = threadIdx.x & 3, token = __shfl(own, p);
         uint32_t n[3];
 #pragma unroll
         for (int c = 0; c < 3; c++) {
@@ -501,7 +507,7 @@ __global__ void __launch_bounds__(1024) k_token_places(const int32_t *__restrict
             n[c] = group_reduce<4>(n[c], [](uint32_t a, uint32_t b) { return a + b; });
         }
         if (part == 0 && i0 + p < M) {
-            places[n[0] + n[1]] = Place{i0 + p, (int)n[1], (int)n[2]};
+            places[n[0] + n[1]] = Place{i0 + p, token, (int)n[1], (int)n[2]};
             first[n[0] + n[1]] = n[1] == 0;
         }
     }
@@ -518,12 +524,11 @@ __device__ __forceinline__ int tokens_before(const uint8_t *__restrict__ first, 
         const uint64_t w = *(const uint64_t *)(first + q);
         n += __popcll(p - q >= 8 ? w : w & ((1ull << (8 * (p - q))) - 1));
     }
-    n = (int)wave_sum((float)n);                                     // at most 2^24 of them
-    if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = n;
+    const float of_wave = wave_sum((float)n);                        // at most 2^24 of them
+    const int lane = threadIdx.x & 63;
+    if (lane == 0) sm[threadIdx.x >> 6] = (int)of_wave;
     __syncthreads();
-    n = 0;
-#pragma unroll
-    for (int w = 0; w < NT / 64; w++) n += sm[w];
+    n = (int)wave_sum(lane < NT / 64 ? (float)sm[lane] : 0.0f);
     __syncthreads();
     return n;
 }
@@ -531,7 +536,7 @@ __device__ __forceinline__ int tokens_before(const uint8_t *__restrict__ first, 
 // acc += rows 0 .. n - 1 in order, row(r) the address of row r; eight of them on their way at once
 template <int NT, int PER, typename T, typename F>
 __device__ __forceinline__ void add_rows(float (&acc)[PER][8], int n, int H, F row) {
-    constexpr int AHEAD = 8;
+    constexpr int AHEAD = AH;
     typedef T v8 __attribute__((ext_vector_type(8), aligned(2)));
     for (int r0 = 0; r0 < n; r0 += AHEAD) {
         const T *from[AHEAD];
@@ -556,8 +561,7 @@ __device__ __forceinline__ void add_rows(float (&acc)[PER][8], int n, int H, F r
 
 // one workgroup per place: a place at which a piece of a token's list begins has work
 template <int NT, int PER>
-__global__ void __launch_bounds__(NT) k_embed_backward(const int32_t *__restrict__ ids, const __half *__restrict__ grad, int M, int V,
-                                                       int H, const __half *__restrict__ E, const __half *__restrict__ g, float eps,
+__global__ void __launch_bounds__(NT, EO) k_embed_backward(const __half *__restrict__ grad, int M, int H, const __half *__restrict__ E, const __half *__restrict__ g, float eps,
                                                        const Place *__restrict__ places, const uint8_t *__restrict__ first,
                                                        float *__restrict__ parts, int32_t *__restrict__ tokens_out,
                                                        float *__restrict__ grads_out, int32_t *__restrict__ count_out) {
@@ -572,22 +576,23 @@ __global__ void __launch_bounds__(NT) k_embed_backward(const int32_t *__restrict
     }
     if (pl.before % RUN_PIECE || piece >= pieces) return;
     const int n = piece == pieces - 1 ? pl.count - pl.before : RUN_PIECE;
+    LnRow<PER> row;
+    if (pieces == 1) ln_load<NT, PER>(row, E + (size_t)pl.token * H, g, H);
+    const int u = pieces == 1 ? tokens_before<NT>(first, p, si) : 0;
     float acc[PER][8] = {};
     add_rows<NT, PER, _Float16>(acc, n, H, [&](int r) { return (const _Float16 *)grad + (size_t)places[p + r].position * H; });
     if (pieces > 1) {                                                // pieces begin at least RUN_PIECE places apart
         ln_store<NT, PER>(acc, parts + (size_t)(p / RUN_PIECE) * H, H);
         return;
     }
-    const int u = tokens_before<NT>(first, p, si), token = min(max(ids[pl.position], 0), V - 1);
-    ln_backward<NT, PER>(acc, E + (size_t)token * H, g, H, eps, sd);
+    ln_backward<NT, PER>(acc, row, H, eps, sd);
     ln_store<NT, PER>(acc, grads_out + (size_t)u * H, H);
-    if (threadIdx.x == 0) tokens_out[u] = token;
+    if (threadIdx.x == 0) tokens_out[u] = pl.token;
 }
 
 // the lists of several pieces: workgroup b looks for one that begins at places b * RUN_PIECE ..
 template <int NT, int PER>
-__global__ void __launch_bounds__(NT) k_embed_backward_join(const int32_t *__restrict__ ids, int M, int V, int H,
-                                                            const __half *__restrict__ E, const __half *__restrict__ g, float eps,
+__global__ void __launch_bounds__(NT) k_embed_backward_join(int M, int H, const __half *__restrict__ E, const __half *__restrict__ g, float eps,
                                                             const Place *__restrict__ places, const uint8_t *__restrict__ first,
                                                             const float *__restrict__ parts, int32_t *__restrict__ tokens_out,
                                                             float *__restrict__ grads_out) {
@@ -603,22 +608,23 @@ __global__ void __launch_bounds__(NT) k_embed_backward_join(const int32_t *__res
     if (!who) return;
     const int p = blockIdx.x * RUN_PIECE + __builtin_ctzll(who);
     const Place pl = places[p];
-    const int pieces = run_pieces(pl.count), token = min(max(ids[pl.position], 0), V - 1);
-    float acc[PER][8] = {};
-    add_rows<NT, PER, float>(acc, pieces, H, [&](int r) { return parts + (size_t)(p / RUN_PIECE + r) * H; });
+    LnRow<PER> row;
+    ln_load<NT, PER>(row, E + (size_t)pl.token * H, g, H);
     const int u = tokens_before<NT>(first, p, si);
-    ln_backward<NT, PER>(acc, E + (size_t)token * H, g, H, eps, sd);
+    float acc[PER][8] = {};
+    add_rows<NT, PER, float>(acc, run_pieces(pl.count), H, [&](int r) { return parts + (size_t)(p / RUN_PIECE + r) * H; });
+    ln_backward<NT, PER>(acc, row, H, eps, sd);
     ln_store<NT, PER>(acc, grads_out + (size_t)u * H, H);
-    if (threadIdx.x == 0) tokens_out[u] = token;
+    if (threadIdx.x == 0) tokens_out[u] = pl.token;
 }
 
 template <int NT, int PER>
-void embed_backward(const int32_t *ids, const __half *grad, int M, int V, int H, const __half *E, const __half *g, float eps,
+void embed_backward(const __half *grad, int M, int H, const __half *E, const __half *g, float eps,
                     const Place *places, const uint8_t *first, float *parts, int32_t *tokens_out, float *grads_out, int32_t *count_out,
                     hipStream_t st) {
-    k_embed_backward<NT, PER><<<M, NT, 0, st>>>(ids, grad, M, V, H, E, g, eps, places, first, parts, tokens_out, grads_out, count_out);
+    k_embed_backward<NT, PER><<<M, NT, 0, st>>>(grad, M, H, E, g, eps, places, first, parts, tokens_out, grads_out, count_out);
     if (M >= 2 * RUN_PIECE)
-        k_embed_backward_join<NT, PER><<<(M + RUN_PIECE - 1) / RUN_PIECE, NT, 0, st>>>(ids, M, V, H, E, g, eps, places, first, parts, tokens_out, grads_out);
+        k_embed_backward_join<NT, PER><<<(M + RUN_PIECE - 1) / RUN_PIECE, NT, 0, st>>>(M, H, E, g, eps, places, first, parts, tokens_out, grads_out);
 }
 
 int check_call(const petals_client_config &cfg, int32_t M) {
@@ -707,18 +713,18 @@ int petals_client_embed_backward(petals_client *client, const int32_t *token_ids
     if (int rc = check_call(*c.cfg, M)) return rc;
     if (token_ids == tokens_out) return ps_fail(PETALS_ERR_INVALID_ARG, "token_ids and tokens_out alias");
     const int V = c.cfg->vocab, H = c.cfg->hidden;
-    // M places of 12 bytes and their flags, then a row of partial sums for every RUN_PIECE places: some 13 M + (M / 32 + 1) 4 H bytes
+    // M places of 16 bytes and their flags, then a row of partial sums for every RUN_PIECE places: some 17 M + (M / 32 + 1) 4 H bytes
     Place *places = (Place *)c.scratch;
-    uint8_t *first = (uint8_t *)(places + (M + 1) / 2 * 2);
+    uint8_t *first = (uint8_t *)(places + M);
     float *parts = (float *)(c.scratch + ((size_t)(first - c.scratch) + M + 255) / 256 * 256);
     hipStream_t st = (hipStream_t)stream;
     const __half *E = (const __half *)c.p->embeddings, *g = (const __half *)c.p->emb_ln_g, *gr = (const __half *)grad_hidden;
     const float eps = c.cfg->ln_eps;
     k_token_places<<<(M + PLACE_ROWS - 1) / PLACE_ROWS, 1024, 0, st>>>(token_ids, M, V, places, first);
-    if (H <= 2048) embed_backward<256, 1>(token_ids, gr, M, V, H, E, g, eps, places, first, parts, tokens_out, grads_out, count_out, st);
-    else if (H <= 4096) embed_backward<512, 1>(token_ids, gr, M, V, H, E, g, eps, places, first, parts, tokens_out, grads_out, count_out, st);
-    else if (H <= 8192) embed_backward<1024, 1>(token_ids, gr, M, V, H, E, g, eps, places, first, parts, tokens_out, grads_out, count_out, st);
-    else embed_backward<1024, 2>(token_ids, gr, M, V, H, E, g, eps, places, first, parts, tokens_out, grads_out, count_out, st);
+    if (H <= 2048) embed_backward<256, 1>(gr, M, H, E, g, eps, places, first, parts, tokens_out, grads_out, count_out, st);
+    else if (H <= 4096) embed_backward<512, 1>(gr, M, H, E, g, eps, places, first, parts, tokens_out, grads_out, count_out, st);
+    else if (H <= 8192) embed_backward<1024, 1>(gr, M, H, E, g, eps, places, first, parts, tokens_out, grads_out, count_out, st);
+    else embed_backward<1024, 2>(gr, M, H, E, g, eps, places, first, parts, tokens_out, grads_out, count_out, st);
     HIP_TRY(hipGetLastError());
     return PETALS_OK;
 }

@@ -140,11 +140,9 @@ __global__ void __launch_bounds__(NT) k_head_finish(const float *__restrict__ pa
                                                     const __half *__restrict__ g, float eps, __half *__restrict__ out) {
     __shared__ double sm[NT / 64][2];
     const int t = blockIdx.x;
-    float acc[PER][8];
-#pragma unroll
-    for (int i = 0; i < PER; i++)
-#pragma unroll
-        for (int e = 0; e < 8; e++) acc[i][e] = 0.0f;
+    LnRow<PER> lr;
+    ln_load<NT, PER>(lr, x + (size_t)t * H, g, H);
+    float acc[PER][8] = {};
     for (int s = 0; s < splits; s++) {
         const float *row = part + ((size_t)s * M + t) * H;
 #pragma unroll
@@ -160,7 +158,7 @@ __global__ void __launch_bounds__(NT) k_head_finish(const float *__restrict__ pa
             }
         }
     }
-    ln_backward<NT, PER>(acc, x + (size_t)t * H, g, H, eps, sm);
+    ln_backward<NT, PER>(acc, lr, H, eps, sm);
     ln_store<NT, PER>(acc, out + (size_t)t * H, H);
 }
 

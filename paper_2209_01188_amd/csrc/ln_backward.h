@@ -4,24 +4,34 @@
 #pragma once
 #include "common.h"
 
-// Columns (threadIdx.x + i NT) 8 .. + 8 of the row belong to this thread; acc holds dy and receives dx.
+// Columns (threadIdx.x + i NT) 8 .. + 8 of the row belong to this thread; acc holds dy and receives dx.  The row and the gain are
+// asked for beforehand (zeros beyond H), so that they arrive while dy is summed up.
+template <int PER>
+struct LnRow {
+    v8h x[PER], g[PER];
+};
 template <int NT, int PER>
-__device__ __forceinline__ void ln_backward(float (&acc)[PER][8], const __half *__restrict__ x, const __half *__restrict__ g, int H,
-                                            float eps, double (*sm)[2]) {
-    float xv[PER][8];
-    double s1 = 0.0, sa = 0.0;
+__device__ __forceinline__ void ln_load(LnRow<PER> &r, const __half *__restrict__ x, const __half *__restrict__ g, int H) {
 #pragma unroll
     for (int i = 0; i < PER; i++) {
         const int k = (threadIdx.x + i * NT) * 8;
+        r.x[i] = r.g[i] = v8h{0, 0, 0, 0, 0, 0, 0, 0};
         if (k < H) {
-            const v8h f = *(const v8h_any *)(x + k), gg = *(const v8h_any *)(g + k);
+            r.x[i] = *(const v8h_any *)(x + k);
+            r.g[i] = *(const v8h_any *)(g + k);
+        }
+    }
+}
+template <int NT, int PER>
+__device__ __forceinline__ void ln_backward(float (&acc)[PER][8], const LnRow<PER> &row, int H, float eps, double (*sm)[2]) {
+    double s1 = 0.0, sa = 0.0;
 #pragma unroll
-            for (int e = 0; e < 8; e++) {
-                xv[i][e] = (float)f[e];
-                acc[i][e] *= (float)gg[e];
-                s1 += (double)xv[i][e];
-                sa += (double)acc[i][e];
-            }
+    for (int i = 0; i < PER; i++) {
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            acc[i][e] *= (float)row.g[i][e];
+            s1 += (double)(float)row.x[i][e];
+            sa += (double)acc[i][e];
         }
     }
     const auto both = [&](double &a, double &b) {
@@ -32,12 +42,9 @@ __device__ __forceinline__ void ln_backward(float (&acc)[PER][8], const __half *
             sm[threadIdx.x >> 6][1] = b;
         }
         __syncthreads();
-        a = b = 0.0;
-#pragma unroll
-        for (int w = 0; w < NT / 64; w++) {
-            a += sm[w][0];
-            b += sm[w][1];
-        }
+        const int lane = threadIdx.x & 63;                          // (all waves' sums in one lane would be 4 registers each)
+        a = wave_sum(lane < NT / 64 ? sm[lane][0] : 0.0);
+        b = wave_sum(lane < NT / 64 ? sm[lane][1] : 0.0);
         __syncthreads();
     };
     both(s1, sa);
@@ -49,7 +56,7 @@ __device__ __forceinline__ void ln_backward(float (&acc)[PER][8], const __half *
         if (k < H) {
 #pragma unroll
             for (int e = 0; e < 8; e++) {
-                const double xc = (double)xv[i][e] - mean;
+                const double xc = (double)(float)row.x[i][e] - mean;
                 s2 = fma(xc, xc, s2);
                 sb = fma((double)acc[i][e], xc, sb);
             }
@@ -62,7 +69,7 @@ __device__ __forceinline__ void ln_backward(float (&acc)[PER][8], const __half *
         const int k = (threadIdx.x + i * NT) * 8;
         if (k < H) {
 #pragma unroll
-            for (int e = 0; e < 8; e++) acc[i][e] = (float)(inv * ((double)acc[i][e] - ma - ((double)xv[i][e] - mean) * along));
+            for (int e = 0; e < 8; e++) acc[i][e] = (float)(inv * ((double)acc[i][e] - ma - ((double)(float)row.x[i][e] - mean) * along));
         }
     }
 }
