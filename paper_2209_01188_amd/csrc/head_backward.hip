@@ -1,5 +1,7 @@
 // Backward of the LM head: da = G E (G fp32 [M, V] the gradient of the logits, E fp16 [V, H] the embedding matrix where the
 // client keeps it), then the derivative of the final LayerNorm.
+#include <mutex>
+
 #include "../../include/petals_finetune.h"
 #include "../../include/petals_span.h"
 #include "client_internal.h"
@@ -67,12 +69,12 @@ __global__ void __launch_bounds__(1024) k_head_pack(const float *__restrict__ G,
 // A wave owns 128 columns of E and walks the rows 32 at a time: a lane loads 8 rows x 8 columns (16 bytes per row; 16 lanes
 // cover 256 consecutive bytes) and turns them around in registers, one byte permutation per word, into the A operands of 8
 // products: product j has columns 8 a + j, a = 0..15.  The token tiles are the B operand.
-template <int MT, bool PAIR>
+template <int MT>
 __global__ void __launch_bounds__(512) k_head_rows(const __half *__restrict__ E, const __half *__restrict__ hi, const __half *__restrict__ lo,
                                                    const float *__restrict__ unit, int M, int V, int H, int KT, int sections, int kt_per,
                                                    float *__restrict__ part) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    const int col = (blockIdx.x * waves + wave) * CHUNK + (lane & 15) * 8, mt0 = blockIdx.z * MT;
+    const int col = (blockIdx.x * waves + wave) * CHUNK + (lane & 15) * 8;
     const int k0 = blockIdx.y * kt_per, k1 = min(KT, k0 + kt_per);
     const __half *Ec = E + min(col, H - 8);
     const int MTT = (M + 15) >> 4;
@@ -83,12 +85,12 @@ __global__ void __launch_bounds__(512) k_head_rows(const __half *__restrict__ E,
         for (int j = 0; j < 8; j++) acc[m][j] = v4f{0, 0, 0, 0};
     float u[MT];
 #pragma unroll
-    for (int m = 0; m < MT; m++) u[m] = unit[(size_t)(min(mt0 + m, MTT - 1) * 16 + (lane & 15)) * sections + k0 / SECTION_KT];
+    for (int m = 0; m < MT; m++) u[m] = unit[(size_t)(min(m, MTT - 1) * 16 + (lane & 15)) * sections + k0 / SECTION_KT];
     for (int kt = k0; kt < k1; kt++) {
         if (kt % SECTION_KT == 0 && kt > k0) {                   // the next section has its own unit
 #pragma unroll
             for (int m = 0; m < MT; m++) {
-                const float next = unit[(size_t)(min(mt0 + m, MTT - 1) * 16 + (lane & 15)) * sections + kt / SECTION_KT], q = u[m] / next;
+                const float next = unit[(size_t)(min(m, MTT - 1) * 16 + (lane & 15)) * sections + kt / SECTION_KT], q = u[m] / next;
 #pragma unroll
                 for (int j = 0; j < 8; j++) acc[m][j] *= q;
                 u[m] = next;
@@ -100,9 +102,9 @@ __global__ void __launch_bounds__(512) k_head_rows(const __half *__restrict__ E,
         v8h b[MT], bl[MT];
 #pragma unroll
         for (int m = 0; m < MT; m++) {
-            const size_t at = (((size_t)min(mt0 + m, MTT - 1) * KT + kt) * 64 + lane) * 8;
+            const size_t at = (((size_t)min(m, MTT - 1) * KT + kt) * 64 + lane) * 8;
             b[m] = *(const v8h *)(hi + at);
-            if (PAIR) bl[m] = *(const v8h *)(lo + at);
+            bl[m] = *(const v8h *)(lo + at);
         }
 #pragma unroll
         for (int j = 0; j < 8; j++) {
@@ -114,7 +116,7 @@ __global__ void __launch_bounds__(512) k_head_rows(const __half *__restrict__ E,
 #pragma unroll
             for (int m = 0; m < MT; m++) {
                 acc[m][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(av, b[m], acc[m][j], 0, 0, 0);
-                if (PAIR) acc[m][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(av, bl[m], acc[m][j], 0, 0, 0);
+                acc[m][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(av, bl[m], acc[m][j], 0, 0, 0);
             }
         }
     }
@@ -122,7 +124,7 @@ __global__ void __launch_bounds__(512) k_head_rows(const __half *__restrict__ E,
     const int c0 = (blockIdx.x * waves + wave) * CHUNK + (lane >> 4) * 32;
 #pragma unroll
     for (int m = 0; m < MT; m++) {
-        const int t = (mt0 + m) * 16 + (lane & 15);
+        const int t = m * 16 + (lane & 15);
         if (t >= M) continue;
         float *o = part + ((size_t)blockIdx.y * M + t) * H + c0;
 #pragma unroll
@@ -130,6 +132,135 @@ __global__ void __launch_bounds__(512) k_head_rows(const __half *__restrict__ E,
             if (c0 + 8 * r >= H) continue;
             *(v4f *)(o + 8 * r) = v4f{acc[m][0][r], acc[m][1][r], acc[m][2][r], acc[m][3][r]} * u[m];
             *(v4f *)(o + 8 * r + 4) = v4f{acc[m][4][r], acc[m][5][r], acc[m][6][r], acc[m][7][r]} * u[m];
+        }
+    }
+}
+
+// Calls of many rows, bound by the matrix instruction: output blocks of BM tokens x 256 columns, 8 waves of BM / 2 x 64.  Token tiles
+// and 32 rows x 512 bytes of E are copied to a ring of 4 slots in LDS, three stages ahead; E's operands are read from there as
+// above (8 rows x 4 columns to a lane) and turned around between the products.
+template <int BM>
+__global__ void __launch_bounds__(512, 2) k_head_block(const __half *__restrict__ E, const __half *__restrict__ G, const float *__restrict__ unit,
+                                                       int M, int V, int H, int KT, int sections, int nb_m, int nb_n, int kt_per,
+                                                       float *__restrict__ part) {
+    constexpr int BN = 256, TM = BM / 32, TN = 4;               // tiles of 16 per wave: tokens, columns
+    constexpr int GT = BM / 16, SLOT = 16384 + GT * 1024, GL = GT / 8, LOADS = 2 + GL;
+    extern __shared__ __align__(16) unsigned char lds[];
+    // workgroup -> block: an XCD (every eighth workgroup) takes a run of blocks of one split, four along the tokens at a time.
+    // (Divisions are done by the vector unit; what is worked out from them is to be scalar all the same.)
+    const int blocks = gridDim.x, xcd = blockIdx.x & 7, per = blocks >> 3, rest = blocks & 7;
+    const int ord = xcd * per + min(xcd, rest) + (blockIdx.x >> 3), split = __builtin_amdgcn_readfirstlane(ord / (nb_m * nb_n)), in = ord - split * nb_m * nb_n;
+    const int strip = __builtin_amdgcn_readfirstlane(in / (4 * nb_n)), wide = min(4, nb_m - 4 * strip), of_strip = in - strip * 4 * nb_n;
+    const int bn = __builtin_amdgcn_readfirstlane(of_strip / wide), bm = strip * 4 + of_strip - bn * wide;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 1, wn = wave >> 1;
+    const int k0 = split * kt_per, k1 = min(KT, k0 + kt_per), MTT = (M + 15) >> 4;
+
+    // what this wave copies per stage: rows 4 wave .. + 4 of E, two per instruction, and GL token tiles.  (The buffer form: rows
+    // behind the matrix come as zeros.)
+    const uint32_t e_off = ((uint32_t)((wave * 4 + (lane >> 5)) * H) + (uint32_t)min(bn * BN + (lane & 31) * 8, H - 8)) * 2;
+    const auto copy = [&](const void *base, uint32_t bytes, uint32_t off, int at) {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)bytes, 0x00020000),
+                                                 (__attribute__((address_space(3))) void *)(lds + at), 16, (int)off, 0, 0, 0);
+    };
+    const auto copies = [&](int kt, int slot) {
+        const int k = min(kt, k1 - 1), v = min(k * 32, V), rows = __builtin_amdgcn_readfirstlane(min(32, V - v));     // (k-tiles that fill up the last four have none)
+#pragma unroll
+        for (int i = 0; i < 2; i++) copy(E + (size_t)v * H, (uint32_t)rows * H * 2, e_off + i * 4u * H, slot * SLOT + (wave * 4 + 2 * i) * 512);
+#pragma unroll
+        for (int i = 0; i < GL; i++)
+            copy(G + ((size_t)min(bm * GT + wave * GL + i, MTT - 1) * KT + k) * 512, 1024, lane * 16, slot * SLOT + 16384 + (wave * GL + i) * 1024);
+    };
+    // operands: row 8 (lane / 16) + i, columns 64 wn + 4 (lane % 16) .. + 4; token tile j
+    const int e_at = (lane >> 4) * 8 * 512 + wn * 128 + (lane & 15) * 8, g_at = 16384 + wm * TM * 1024 + lane * 16;
+    const auto read_e = [&](int slot, int i) { return *(const v2i *)(lds + slot * SLOT + e_at + i * 512); };
+    const auto read_g = [&](int slot, int j) { return *(const v8h *)(lds + slot * SLOT + g_at + j * 1024); };
+
+    v4f acc[TN][TM];
+#pragma unroll
+    for (int i = 0; i < TN; i++)
+#pragma unroll
+        for (int j = 0; j < TM; j++) acc[i][j] = v4f{0, 0, 0, 0};
+    float u[TM];
+    const uint32_t u_off = (lane & 15) * sections;
+    const auto unit_of = [&](int j, int kt) { return (unit + ((size_t)min(bm * GT + wm * TM + j, MTT - 1) * 16 * sections + kt / SECTION_KT))[u_off]; };
+#pragma unroll
+    for (int j = 0; j < TM; j++) u[j] = unit_of(j, k0);
+
+#pragma unroll
+    for (int s = 0; s < 4; s++) copies(k0 + s, s);
+    v2i fe[2][8];
+    v8h fg[2][TM];
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * LOADS) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 8; i++) fe[0][i] = read_e(0, i);
+#pragma unroll
+    for (int j = 0; j < TM; j++) fg[0][j] = read_g(0, j);
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * LOADS) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+
+    // Stage kt: its operands are in registers, everybody has read slot kt % 4, and everybody's copies for stage kt + 1 have
+    // landed.  Beside the products, the copies of kt + 4 are requested and the operands of kt + 1 read, a few at a time.
+    const auto stage = [&](int kt, auto S) {
+        constexpr int s = decltype(S)::value, cur = s & 1, nxt = cur ^ 1, next_slot = (s + 1) & 3;
+#pragma unroll
+        for (int i = 0; i < TN; i++) {
+            v4i a;
+#pragma unroll
+            for (int w = 0; w < 4; w++)
+                a[w] = (int)__builtin_amdgcn_perm((uint32_t)fe[cur][2 * w + 1][i >> 1], (uint32_t)fe[cur][2 * w][i >> 1], i & 1 ? 0x07060302 : 0x05040100);
+            const v8h av = *(const v8h *)&a;
+#pragma unroll
+            for (int j = 0; j < TM; j++) {
+                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(av, fg[cur][j], acc[i][j], 0, 0, 0);
+                if (j == TM / 2 - 1 || j == TM - 1) {
+                    const int at = 2 * i + (j == TM - 1);        // half a row of products done: 0 .. 7
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (at == 0) copies(kt + 4, s);
+                    if (at == 1 || at == 2) {
+#pragma unroll
+                        for (int r = 0; r < 4; r++) fe[nxt][4 * (at - 1) + r] = read_e(next_slot, 4 * (at - 1) + r);
+                    }
+                    if (at == 3 || at == 4) {
+#pragma unroll
+                        for (int r = 0; r < TM / 2; r++) fg[nxt][TM / 2 * (at - 3) + r] = read_g(next_slot, TM / 2 * (at - 3) + r);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        }
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * LOADS) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    for (int kt = k0; kt < k1; kt += 4) {
+        if (kt % SECTION_KT == 0 && kt > k0) {                   // the next section has its own unit
+#pragma unroll
+            for (int j = 0; j < TM; j++) {
+                const float next = unit_of(j, kt), ratio = u[j] / next;
+#pragma unroll
+                for (int i = 0; i < TN; i++) acc[i][j] *= ratio;
+                u[j] = next;
+            }
+        }
+        stage(kt, std::integral_constant<int, 0>());
+        stage(kt + 1, std::integral_constant<int, 1>());
+        stage(kt + 2, std::integral_constant<int, 2>());
+        stage(kt + 3, std::integral_constant<int, 3>());
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // nothing may land in LDS after the workgroup's end
+    // result register r of tile (i, j): token lane % 16, column 4 (4 (lane / 16) + r) + i of the wave's
+#pragma unroll
+    for (int j = 0; j < TM; j++) {
+        const int t = (bm * GT + wm * TM + j) * 16 + (lane & 15);
+        if (t >= M) continue;
+        float *o = part + ((size_t)split * M + t) * H;
+#pragma unroll
+        for (int r = 0; r < 4; r++) {
+            const int c = bn * BN + wn * 64 + (lane >> 4) * 16 + r * 4;
+            if (c < H) *(v4f *)(o + c) = v4f{acc[0][j][r], acc[1][j][r], acc[2][j][r], acc[3][j][r]} * u[j];
         }
     }
 }
@@ -164,23 +295,33 @@ __global__ void __launch_bounds__(NT) k_head_finish(const float *__restrict__ pa
 
 // How a call of M rows is cut up, and where things lie in its store
 struct HeadPlan {
-    int mtt, kt, sections;           // token tiles, k-tiles, sections of a row
+    int mtt, kt, sections;           // token tiles, k-tiles (a multiple of 4), sections of a row
     bool pair;
-    int mt, waves, groups, kt_per, splits;
+    int mt, waves, groups;           // few rows: token tiles of a wave, waves of a workgroup, workgroups along the columns
+    int bm, nb_m, nb_n;              // many rows: tokens of a block, blocks
+    int kt_per, splits;
     size_t hi, lo, unit, part, bytes;
 };
 HeadPlan head_plan(const petals_client_config &cfg, int M) {
     HeadPlan p;
     p.mtt = (M + 15) / 16;
-    p.kt = (cfg.vocab + 31) / 32;
+    p.kt = (cfg.vocab + 127) / 128 * 4;
     p.sections = (cfg.vocab + SECTION - 1) / SECTION;
     p.pair = M <= PETALS_HEAD_BACKWARD_PAIR_ROWS;
-    p.mt = p.mtt >= 4 ? 4 : p.mtt == 3 ? 4 : p.mtt;
-    const int chunks = (cfg.hidden + CHUNK - 1) / CHUNK;
-    p.groups = (chunks + 7) / 8;
-    p.waves = (chunks + p.groups - 1) / p.groups;
-    const int want = max(1, 512 / (p.groups * ((p.mtt + p.mt - 1) / p.mt)));
-    p.kt_per = max(4, (p.kt + want - 1) / want);
+    int want;
+    if (p.pair) {
+        p.mt = p.mtt >= 3 ? 4 : p.mtt;
+        const int chunks = (cfg.hidden + CHUNK - 1) / CHUNK;
+        p.groups = (chunks + 7) / 8;
+        p.waves = (chunks + p.groups - 1) / p.groups;
+        want = max(1, 512 / p.groups);
+    } else {
+        p.bm = (M + 127) / 128 * 128 < (M + 255) / 256 * 256 ? 128 : 256;
+        p.nb_m = (M + p.bm - 1) / p.bm;
+        p.nb_n = (cfg.hidden + 255) / 256;
+        want = max(1, 256 / (p.nb_m * p.nb_n));
+    }
+    p.kt_per = max(4, (p.kt / 4 + want - 1) / want * 4);
     p.splits = (p.kt + p.kt_per - 1) / p.kt_per;
     const size_t tiles = ps_align_up((size_t)p.mtt * p.kt * 1024);
     p.hi = 0;
@@ -193,12 +334,25 @@ HeadPlan head_plan(const petals_client_config &cfg, int M) {
 
 template <int MT>
 void head_rows(const HeadPlan &p, const __half *E, uint8_t *store, int M, int V, int H, hipStream_t st) {
-    const dim3 grid(p.groups, p.splits, (p.mtt + MT - 1) / MT);
-    const __half *hi = (const __half *)(store + p.hi), *lo = (const __half *)(store + p.lo);
-    const float *unit = (const float *)(store + p.unit);
-    float *part = (float *)(store + p.part);
-    if (p.pair) k_head_rows<MT, true><<<grid, 64 * p.waves, 0, st>>>(E, hi, lo, unit, M, V, H, p.kt, p.sections, p.kt_per, part);
-    else k_head_rows<MT, false><<<grid, 64 * p.waves, 0, st>>>(E, hi, lo, unit, M, V, H, p.kt, p.sections, p.kt_per, part);
+    k_head_rows<MT><<<dim3(p.groups, p.splits), 64 * p.waves, 0, st>>>(E, (const __half *)(store + p.hi), (const __half *)(store + p.lo),
+                                                                      (const float *)(store + p.unit), M, V, H, p.kt, p.sections, p.kt_per,
+                                                                      (float *)(store + p.part));
+}
+template <int BM>
+hipError_t head_block(const HeadPlan &p, const __half *E, uint8_t *store, int M, int V, int H, hipStream_t st) {
+    constexpr int bytes = 4 * (16384 + BM / 16 * 1024);
+    {   // the limit belongs to the function, for the whole process
+        static std::mutex attr_lock;
+        static bool attr_set = false;
+        std::lock_guard<std::mutex> hold(attr_lock);
+        if (!attr_set) {
+            if (hipError_t e = hipFuncSetAttribute((const void *)k_head_block<BM>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes)) return e;
+            attr_set = true;
+        }
+    }
+    k_head_block<BM><<<p.nb_m * p.nb_n * p.splits, 512, bytes, st>>>(E, (const __half *)(store + p.hi), (const float *)(store + p.unit), M, V, H, p.kt,
+                                                                    p.sections, p.nb_m, p.nb_n, p.kt_per, (float *)(store + p.part));
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -233,10 +387,14 @@ int petals_client_lm_head_backward(petals_client *client, void *dev_store, const
     k_head_pack<<<dim3(p.sections, p.mtt), 1024, 0, st>>>(grad_logits, M, V, p.kt, p.sections, (__half *)(store + p.hi),
                                                           p.pair ? (__half *)(store + p.lo) : nullptr, (float *)(store + p.unit));
     HIP_TRY(hipGetLastError());
-    if (p.mt == 1) head_rows<1>(p, E, store, M, V, H, st);
-    else if (p.mt == 2) head_rows<2>(p, E, store, M, V, H, st);
-    else head_rows<4>(p, E, store, M, V, H, st);
-    HIP_TRY(hipGetLastError());
+    if (p.pair) {
+        if (p.mt == 1) head_rows<1>(p, E, store, M, V, H, st);
+        else if (p.mt == 2) head_rows<2>(p, E, store, M, V, H, st);
+        else head_rows<4>(p, E, store, M, V, H, st);
+        HIP_TRY(hipGetLastError());
+    } else {
+        HIP_TRY(p.bm == 128 ? head_block<128>(p, E, store, M, V, H, st) : head_block<256>(p, E, store, M, V, H, st));
+    }
     if (H <= 2048) k_head_finish<256, 1><<<M, 256, 0, st>>>(part, p.splits, M, H, x, g, c.cfg->ln_eps, out);
     else if (H <= 4096) k_head_finish<512, 1><<<M, 512, 0, st>>>(part, p.splits, M, H, x, g, c.cfg->ln_eps, out);
     else if (H <= 8192) k_head_finish<1024, 1><<<M, 1024, 0, st>>>(part, p.splits, M, H, x, g, c.cfg->ln_eps, out);
