@@ -9,12 +9,6 @@
 #include "host_util.h"
 #include "ln_backward.h"
 
-#ifndef AH
-#define AH 4
-#endif
-#ifndef EO
-#define EO 1
-#endif
 namespace {
 
 // ------------------------------------------------------------------------------------ a row's softmax statistics
@@ -533,35 +527,9 @@ __device__ __forceinline__ int tokens_before(const uint8_t *__restrict__ first, 
     return n;
 }
 
-// acc += rows 0 .. n - 1 in order, row(r) the address of row r; eight of them on their way at once
-template <int NT, int PER, typename T, typename F>
-__device__ __forceinline__ void add_rows(float (&acc)[PER][8], int n, int H, F row) {
-    constexpr int AHEAD = AH;
-    typedef T v8 __attribute__((ext_vector_type(8), aligned(2)));
-    for (int r0 = 0; r0 < n; r0 += AHEAD) {
-        const T *from[AHEAD];
-#pragma unroll
-        for (int u = 0; u < AHEAD; u++) from[u] = row(min(r0 + u, n - 1));
-#pragma unroll
-        for (int i = 0; i < PER; i++) {
-            const int k = (threadIdx.x + i * NT) * 8;
-            if (k >= H) continue;
-            v8 f[AHEAD];
-#pragma unroll
-            for (int u = 0; u < AHEAD; u++) f[u] = *(const v8 *)(from[u] + k);
-#pragma unroll
-            for (int u = 0; u < AHEAD; u++)
-                if (r0 + u < n) {
-#pragma unroll
-                    for (int e = 0; e < 8; e++) acc[i][e] += (float)f[u][e];
-                }
-        }
-    }
-}
-
 // one workgroup per place: a place at which a piece of a token's list begins has work
 template <int NT, int PER>
-__global__ void __launch_bounds__(NT, EO) k_embed_backward(const __half *__restrict__ grad, int M, int H, const __half *__restrict__ E, const __half *__restrict__ g, float eps,
+__global__ void __launch_bounds__(NT) k_embed_backward(const __half *__restrict__ grad, int M, int H, const __half *__restrict__ E, const __half *__restrict__ g, float eps,
                                                        const Place *__restrict__ places, const uint8_t *__restrict__ first,
                                                        float *__restrict__ parts, int32_t *__restrict__ tokens_out,
                                                        float *__restrict__ grads_out, int32_t *__restrict__ count_out) {

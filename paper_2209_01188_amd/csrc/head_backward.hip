@@ -14,25 +14,27 @@ namespace {
 
 constexpr int SECTION = 4096;              // columns of G that share a row's scale
 constexpr int SECTION_KT = SECTION / 32;   // in k-tiles
-constexpr int CHUNK = 128;                 // columns of E that a wave owns
 typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));     // rows of an odd vocabulary begin anywhere
 
 // G as fp16 in the operand order of v_mfma_f32_16x16x32_f16: tile (mt, kt) of 16 rows x 32 columns is 1 KB, lane slot
 // 16 (column / 8) + row holds 8 columns.  A row's section is scaled so that its largest value becomes 32768: fp16 then keeps
 // 2^-12 of a value down to 2^-29 of the largest (a softmax's gradient reaches from 1 down to 1e-9 and less), and the largest,
 // mostly the label's, exactly.  lo (may be null): what the rounding left, in the same scale.
-// One workgroup per 16 rows and section, a wave per row.
-__global__ void __launch_bounds__(1024) k_head_pack(const float *__restrict__ G, int M, int V, int KT, int sections,
-                                                    __half *__restrict__ hi, __half *__restrict__ lo, float *__restrict__ unit) {
-    const int sec = blockIdx.x, mt = blockIdx.y, lane = threadIdx.x & 63, r = threadIdx.x >> 6, t = mt * 16 + r;
-    float f[SECTION / 512][8];
+// One workgroup per 16 rows and section; a wave reads PACK_TILES of its tiles, whole lines of 128 bytes, and stores them as they
+// are laid out.
+constexpr int PACK_WAVES = 16, PACK_TILES = SECTION_KT / PACK_WAVES;
+__global__ void __launch_bounds__(64 * PACK_WAVES) k_head_pack(const float *__restrict__ G, int M, int V, int KT, int sections,
+                                                               __half *__restrict__ hi, __half *__restrict__ lo, float *__restrict__ unit) {
+    __shared__ float most[16][PACK_WAVES];
+    const int sec = blockIdx.x, mt = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, t = mt * 16 + r;
+    const float *row = G + (size_t)min(t, M - 1) * V;
+    float f[PACK_TILES][8];
     float mx = 0.0f;
 #pragma unroll
-    for (int i = 0; i < SECTION / 512; i++) {
-        const int v = sec * SECTION + i * 512 + lane * 8;
-        const float *row = G + (size_t)min(t, M - 1) * V;
-        if (v + 7 < V) {
-            const v4f a = *(const v4f_any *)(row + v), b = *(const v4f_any *)(row + v + 4);
+    for (int i = 0; i < PACK_TILES; i++) {
+        const int kt = sec * SECTION_KT + wave * PACK_TILES + i, v = kt * 32 + (lane >> 4) * 8;
+        if (kt * 32 + 32 <= V) {
+            const v4f a = __builtin_nontemporal_load((const v4f_any *)(row + v)), b = __builtin_nontemporal_load((const v4f_any *)(row + v + 4));
 #pragma unroll
             for (int e = 0; e < 4; e++) {
                 f[i][e] = a[e];
@@ -42,109 +44,50 @@ __global__ void __launch_bounds__(1024) k_head_pack(const float *__restrict__ G,
 #pragma unroll
             for (int e = 0; e < 8; e++) f[i][e] = v + e < V ? row[v + e] : 0.0f;
         }
+    }
+#pragma unroll
+    for (int i = 0; i < PACK_TILES; i++)
 #pragma unroll
         for (int e = 0; e < 8; e++) mx = fmaxf(mx, fabsf(f[i][e]));
-    }
-    mx = t < M ? wave_max(mx) : 0.0f;
-    // (sections of zeros and of next to nothing: a unit of 2^-60, so that the ratio of two units stays a number)
-    const float u = fmaxf(mx * 0x1p-15f, 0x1p-60f), s = 1.0f / u;
-    if (lane == 0) unit[(size_t)t * sections + sec] = u;
+    mx = fmaxf(mx, __shfl_xor(mx, 16));
+    mx = fmaxf(mx, __shfl_xor(mx, 32));
+    if (lane < 16) most[r][wave] = mx;
+    __syncthreads();
+    mx = 0.0f;
 #pragma unroll
-    for (int i = 0; i < SECTION / 512; i++) {
-        const int kt = sec * SECTION_KT + i * 16 + (lane >> 2);
-        if (kt >= KT) continue;
+    for (int w = 0; w < PACK_WAVES; w++) mx = fmaxf(mx, most[r][w]);
+    // (rows behind the call's, sections of zeros and of next to nothing: a unit of 2^-60, so that the ratio of two units stays a number)
+    const float u = t < M ? fmaxf(mx * 0x1p-15f, 0x1p-60f) : 0x1p-60f, s = t < M ? 1.0f / u : 0.0f;
+    if (threadIdx.x < 16) unit[(size_t)t * sections + sec] = u;
+#pragma unroll
+    for (int i = 0; i < PACK_TILES; i++) {
+        const int kt = sec * SECTION_KT + wave * PACK_TILES + i;
+        if (kt >= KT) break;
         v8h h, l;
 #pragma unroll
         for (int e = 0; e < 8; e++) {
-            const float x = t < M ? f[i][e] * s : 0.0f;
+            const float x = f[i][e] * s;
             h[e] = (_Float16)x;
             l[e] = (_Float16)(x - (float)h[e]);
         }
-        const size_t at = (((size_t)mt * KT + kt) * 64 + (lane & 3) * 16 + r) * 8;
+        const size_t at = (((size_t)mt * KT + kt) * 64 + lane) * 8;
         *(v8h *)(hi + at) = h;
         if (lo) *(v8h *)(lo + at) = l;
     }
 }
 
-// A wave owns 128 columns of E and walks the rows 32 at a time: a lane loads 8 rows x 8 columns (16 bytes per row; 16 lanes
-// cover 256 consecutive bytes) and turns them around in registers, one byte permutation per word, into the A operands of 8
-// products: product j has columns 8 a + j, a = 0..15.  The token tiles are the B operand.
-template <int MT>
-__global__ void __launch_bounds__(512) k_head_rows(const __half *__restrict__ E, const __half *__restrict__ hi, const __half *__restrict__ lo,
-                                                   const float *__restrict__ unit, int M, int V, int H, int KT, int sections, int kt_per,
-                                                   float *__restrict__ part) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    const int col = (blockIdx.x * waves + wave) * CHUNK + (lane & 15) * 8;
-    const int k0 = blockIdx.y * kt_per, k1 = min(KT, k0 + kt_per);
-    const __half *Ec = E + min(col, H - 8);
-    const int MTT = (M + 15) >> 4;
-    v4f acc[MT][8];
-#pragma unroll
-    for (int m = 0; m < MT; m++)
-#pragma unroll
-        for (int j = 0; j < 8; j++) acc[m][j] = v4f{0, 0, 0, 0};
-    float u[MT];
-#pragma unroll
-    for (int m = 0; m < MT; m++) u[m] = unit[(size_t)(min(m, MTT - 1) * 16 + (lane & 15)) * sections + k0 / SECTION_KT];
-    for (int kt = k0; kt < k1; kt++) {
-        if (kt % SECTION_KT == 0 && kt > k0) {                   // the next section has its own unit
-#pragma unroll
-            for (int m = 0; m < MT; m++) {
-                const float next = unit[(size_t)(min(m, MTT - 1) * 16 + (lane & 15)) * sections + kt / SECTION_KT], q = u[m] / next;
-#pragma unroll
-                for (int j = 0; j < 8; j++) acc[m][j] *= q;
-                u[m] = next;
-            }
-        }
-        v4i r[8];
-#pragma unroll
-        for (int i = 0; i < 8; i++) r[i] = *(const v4i *)(Ec + (size_t)min(kt * 32 + (lane >> 4) * 8 + i, V - 1) * H);
-        v8h b[MT], bl[MT];
-#pragma unroll
-        for (int m = 0; m < MT; m++) {
-            const size_t at = (((size_t)min(m, MTT - 1) * KT + kt) * 64 + lane) * 8;
-            b[m] = *(const v8h *)(hi + at);
-            bl[m] = *(const v8h *)(lo + at);
-        }
-#pragma unroll
-        for (int j = 0; j < 8; j++) {
-            v4i a;
-#pragma unroll
-            for (int w = 0; w < 4; w++)
-                a[w] = (int)__builtin_amdgcn_perm((uint32_t)r[2 * w + 1][j >> 1], (uint32_t)r[2 * w][j >> 1], j & 1 ? 0x07060302 : 0x05040100);
-            const v8h av = *(const v8h *)&a;
-#pragma unroll
-            for (int m = 0; m < MT; m++) {
-                acc[m][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(av, b[m], acc[m][j], 0, 0, 0);
-                acc[m][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(av, bl[m], acc[m][j], 0, 0, 0);
-            }
-        }
-    }
-    // result register r of product j: token lane % 16, column 8 (4 (lane / 16) + r) + j of the wave's
-    const int c0 = (blockIdx.x * waves + wave) * CHUNK + (lane >> 4) * 32;
-#pragma unroll
-    for (int m = 0; m < MT; m++) {
-        const int t = m * 16 + (lane & 15);
-        if (t >= M) continue;
-        float *o = part + ((size_t)blockIdx.y * M + t) * H + c0;
-#pragma unroll
-        for (int r = 0; r < 4; r++) {
-            if (c0 + 8 * r >= H) continue;
-            *(v4f *)(o + 8 * r) = v4f{acc[m][0][r], acc[m][1][r], acc[m][2][r], acc[m][3][r]} * u[m];
-            *(v4f *)(o + 8 * r + 4) = v4f{acc[m][4][r], acc[m][5][r], acc[m][6][r], acc[m][7][r]} * u[m];
-        }
-    }
-}
-
-// Calls of many rows, bound by the matrix instruction: output blocks of BM tokens x 256 columns, 8 waves of BM / 2 x 64.  Token tiles
-// and 32 rows x 512 bytes of E are copied to a ring of 4 slots in LDS, three stages ahead; E's operands are read from there as
-// above (8 rows x 4 columns to a lane) and turned around between the products.
-template <int BM>
-__global__ void __launch_bounds__(512, 2) k_head_block(const __half *__restrict__ E, const __half *__restrict__ G, const float *__restrict__ unit,
-                                                       int M, int V, int H, int KT, int sections, int nb_m, int nb_n, int kt_per,
-                                                       float *__restrict__ part) {
+// The product: output blocks of BM tokens x 256 columns, 8 waves of BM / 2 x 64, the contraction over the vocabulary split over
+// workgroups until every compute unit has one.  Token tiles and 32 rows x 512 bytes of E are copied to a ring of 4 slots in LDS,
+// three stages ahead.  The contraction runs along E's columns in memory, so its operands are turned around: a lane reads 4 columns
+// of 8 rows and makes of them, one byte permutation per word, the A operands of 4 products (product i has columns 4 a + i).
+// PAIR: the token tiles twice, G's values and what their rounding left; calls of up to 64 rows, which wait for E's bytes anyway.
+template <int BM, bool PAIR>
+__global__ void __launch_bounds__(512, 2) k_head_block(const __half *__restrict__ E, const __half *__restrict__ hi, const __half *__restrict__ lo,
+                                                       const float *__restrict__ unit, int M, int V, int H, int KT, int sections, int nb_m,
+                                                       int nb_n, int kt_per, float *__restrict__ part) {
     constexpr int BN = 256, TM = BM / 32, TN = 4;               // tiles of 16 per wave: tokens, columns
-    constexpr int GT = BM / 16, SLOT = 16384 + GT * 1024, GL = GT / 8, LOADS = 2 + GL;
+    constexpr int GT = BM / 16, GS = PAIR ? 8 : GT, SLOT = 16384 + GS * 1024, GL = GS / 8, LOADS = 2 + GL;
+    static_assert(GS % 8 == 0 && (!PAIR || 2 * GT <= 8), "as many token tiles to copy for every wave");
     extern __shared__ __align__(16) unsigned char lds[];
     // workgroup -> block: an XCD (every eighth workgroup) takes a run of blocks of one split, four along the tokens at a time.
     // (Divisions are done by the vector unit; what is worked out from them is to be scalar all the same.)
@@ -168,12 +111,16 @@ __global__ void __launch_bounds__(512, 2) k_head_block(const __half *__restrict_
         for (int i = 0; i < 2; i++) copy(E + (size_t)v * H, (uint32_t)rows * H * 2, e_off + i * 4u * H, slot * SLOT + (wave * 4 + 2 * i) * 512);
 #pragma unroll
         for (int i = 0; i < GL; i++)
-            copy(G + ((size_t)min(bm * GT + wave * GL + i, MTT - 1) * KT + k) * 512, 1024, lane * 16, slot * SLOT + 16384 + (wave * GL + i) * 1024);
+        {   // (fewer than 8 tiles of a pair: some waves copy one that nobody reads)
+            const int tile = wave * GL + i;
+            copy((PAIR && tile >= GT ? lo : hi) + ((size_t)min(bm * GT + (PAIR ? tile % GT : tile), MTT - 1) * KT + k) * 512, 1024, lane * 16,
+                 slot * SLOT + 16384 + tile * 1024);
+        }
     };
     // operands: row 8 (lane / 16) + i, columns 64 wn + 4 (lane % 16) .. + 4; token tile j
     const int e_at = (lane >> 4) * 8 * 512 + wn * 128 + (lane & 15) * 8, g_at = 16384 + wm * TM * 1024 + lane * 16;
     const auto read_e = [&](int slot, int i) { return *(const v2i *)(lds + slot * SLOT + e_at + i * 512); };
-    const auto read_g = [&](int slot, int j) { return *(const v8h *)(lds + slot * SLOT + g_at + j * 1024); };
+    const auto read_g = [&](int slot, int j) { return *(const v8h *)(lds + slot * SLOT + g_at + (j < TM ? j : GT + j - TM) * 1024); };
 
     v4f acc[TN][TM];
 #pragma unroll
@@ -189,14 +136,15 @@ __global__ void __launch_bounds__(512, 2) k_head_block(const __half *__restrict_
 #pragma unroll
     for (int s = 0; s < 4; s++) copies(k0 + s, s);
     v2i fe[2][8];
-    v8h fg[2][TM];
+    constexpr int NG = PAIR ? 2 * TM : TM;
+    v8h fg[2][NG];
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * LOADS) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 #pragma unroll
     for (int i = 0; i < 8; i++) fe[0][i] = read_e(0, i);
 #pragma unroll
-    for (int j = 0; j < TM; j++) fg[0][j] = read_g(0, j);
+    for (int j = 0; j < NG; j++) fg[0][j] = read_g(0, j);
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * LOADS) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
@@ -205,6 +153,19 @@ __global__ void __launch_bounds__(512, 2) k_head_block(const __half *__restrict_
     // landed.  Beside the products, the copies of kt + 4 are requested and the operands of kt + 1 read, a few at a time.
     const auto stage = [&](int kt, auto S) {
         constexpr int s = decltype(S)::value, cur = s & 1, nxt = cur ^ 1, next_slot = (s + 1) & 3;
+        const auto beside = [&](int at) {                        // after eighth `at` of the products
+            __builtin_amdgcn_sched_barrier(0);
+            if (at == 0) copies(kt + 4, s);
+            if (at == 1 || at == 2) {
+#pragma unroll
+                for (int r = 0; r < 4; r++) fe[nxt][4 * (at - 1) + r] = read_e(next_slot, 4 * (at - 1) + r);
+            }
+            if (at == 3 || at == 4) {
+#pragma unroll
+                for (int r = at == 3 ? 0 : (NG + 1) / 2; r < (at == 3 ? (NG + 1) / 2 : NG); r++) fg[nxt][r] = read_g(next_slot, r);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
 #pragma unroll
         for (int i = 0; i < TN; i++) {
             v4i a;
@@ -215,20 +176,9 @@ __global__ void __launch_bounds__(512, 2) k_head_block(const __half *__restrict_
 #pragma unroll
             for (int j = 0; j < TM; j++) {
                 acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(av, fg[cur][j], acc[i][j], 0, 0, 0);
-                if (j == TM / 2 - 1 || j == TM - 1) {
-                    const int at = 2 * i + (j == TM - 1);        // half a row of products done: 0 .. 7
-                    __builtin_amdgcn_sched_barrier(0);
-                    if (at == 0) copies(kt + 4, s);
-                    if (at == 1 || at == 2) {
-#pragma unroll
-                        for (int r = 0; r < 4; r++) fe[nxt][4 * (at - 1) + r] = read_e(next_slot, 4 * (at - 1) + r);
-                    }
-                    if (at == 3 || at == 4) {
-#pragma unroll
-                        for (int r = 0; r < TM / 2; r++) fg[nxt][TM / 2 * (at - 3) + r] = read_g(next_slot, TM / 2 * (at - 3) + r);
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+                if constexpr (PAIR) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(av, fg[cur][TM + j], acc[i][j], 0, 0, 0);
+                if (TM == 1 || j == TM / 2 - 1) beside(2 * i);
+                if (j == TM - 1) beside(2 * i + 1);
             }
         }
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * LOADS) : "memory");
@@ -274,21 +224,7 @@ __global__ void __launch_bounds__(NT) k_head_finish(const float *__restrict__ pa
     LnRow<PER> lr;
     ln_load<NT, PER>(lr, x + (size_t)t * H, g, H);
     float acc[PER][8] = {};
-    for (int s = 0; s < splits; s++) {
-        const float *row = part + ((size_t)s * M + t) * H;
-#pragma unroll
-        for (int i = 0; i < PER; i++) {
-            const int k = (threadIdx.x + i * NT) * 8;
-            if (k < H) {
-#pragma unroll
-                for (int h = 0; h < 2; h++) {
-                    const v4f f = *(const v4f *)(row + k + 4 * h);
-#pragma unroll
-                    for (int e = 0; e < 4; e++) acc[i][4 * h + e] += f[e];
-                }
-            }
-        }
-    }
+    add_rows<NT, PER, float>(acc, splits, H, [&](int s) { return part + ((size_t)s * M + t) * H; });
     ln_backward<NT, PER>(acc, lr, H, eps, sm);
     ln_store<NT, PER>(acc, out + (size_t)t * H, H);
 }
@@ -297,8 +233,7 @@ __global__ void __launch_bounds__(NT) k_head_finish(const float *__restrict__ pa
 struct HeadPlan {
     int mtt, kt, sections;           // token tiles, k-tiles (a multiple of 4), sections of a row
     bool pair;
-    int mt, waves, groups;           // few rows: token tiles of a wave, waves of a workgroup, workgroups along the columns
-    int bm, nb_m, nb_n;              // many rows: tokens of a block, blocks
+    int bm, nb_m, nb_n;              // tokens of a block, blocks
     int kt_per, splits;
     size_t hi, lo, unit, part, bytes;
 };
@@ -308,19 +243,10 @@ HeadPlan head_plan(const petals_client_config &cfg, int M) {
     p.kt = (cfg.vocab + 127) / 128 * 4;
     p.sections = (cfg.vocab + SECTION - 1) / SECTION;
     p.pair = M <= PETALS_HEAD_BACKWARD_PAIR_ROWS;
-    int want;
-    if (p.pair) {
-        p.mt = p.mtt >= 3 ? 4 : p.mtt;
-        const int chunks = (cfg.hidden + CHUNK - 1) / CHUNK;
-        p.groups = (chunks + 7) / 8;
-        p.waves = (chunks + p.groups - 1) / p.groups;
-        want = max(1, 512 / p.groups);
-    } else {
-        p.bm = (M + 127) / 128 * 128 < (M + 255) / 256 * 256 ? 128 : 256;
-        p.nb_m = (M + p.bm - 1) / p.bm;
-        p.nb_n = (cfg.hidden + 255) / 256;
-        want = max(1, 256 / (p.nb_m * p.nb_n));
-    }
+    p.bm = M <= 32 ? 32 : M <= 64 ? 64 : (M + 127) / 128 * 128 < (M + 255) / 256 * 256 ? 128 : 256;
+    p.nb_m = (M + p.bm - 1) / p.bm;
+    p.nb_n = (cfg.hidden + 255) / 256;
+    const int want = max(1, 256 / (p.nb_m * p.nb_n));
     p.kt_per = max(4, (p.kt / 4 + want - 1) / want * 4);
     p.splits = (p.kt + p.kt_per - 1) / p.kt_per;
     const size_t tiles = ps_align_up((size_t)p.mtt * p.kt * 1024);
@@ -332,26 +258,21 @@ HeadPlan head_plan(const petals_client_config &cfg, int M) {
     return p;
 }
 
-template <int MT>
-void head_rows(const HeadPlan &p, const __half *E, uint8_t *store, int M, int V, int H, hipStream_t st) {
-    k_head_rows<MT><<<dim3(p.groups, p.splits), 64 * p.waves, 0, st>>>(E, (const __half *)(store + p.hi), (const __half *)(store + p.lo),
-                                                                      (const float *)(store + p.unit), M, V, H, p.kt, p.sections, p.kt_per,
-                                                                      (float *)(store + p.part));
-}
-template <int BM>
+template <int BM, bool PAIR>
 hipError_t head_block(const HeadPlan &p, const __half *E, uint8_t *store, int M, int V, int H, hipStream_t st) {
-    constexpr int bytes = 4 * (16384 + BM / 16 * 1024);
+    constexpr int bytes = 4 * (16384 + (PAIR ? 8 : BM / 16) * 1024);
     {   // the limit belongs to the function, for the whole process
         static std::mutex attr_lock;
         static bool attr_set = false;
         std::lock_guard<std::mutex> hold(attr_lock);
         if (!attr_set) {
-            if (hipError_t e = hipFuncSetAttribute((const void *)k_head_block<BM>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes)) return e;
+            if (hipError_t e = hipFuncSetAttribute((const void *)k_head_block<BM, PAIR>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes)) return e;
             attr_set = true;
         }
     }
-    k_head_block<BM><<<p.nb_m * p.nb_n * p.splits, 512, bytes, st>>>(E, (const __half *)(store + p.hi), (const float *)(store + p.unit), M, V, H, p.kt,
-                                                                    p.sections, p.nb_m, p.nb_n, p.kt_per, (float *)(store + p.part));
+    k_head_block<BM, PAIR><<<p.nb_m * p.nb_n * p.splits, 512, bytes, st>>>(E, (const __half *)(store + p.hi), (const __half *)(store + p.lo),
+                                                                          (const float *)(store + p.unit), M, V, H, p.kt, p.sections, p.nb_m,
+                                                                          p.nb_n, p.kt_per, (float *)(store + p.part));
     return hipGetLastError();
 }
 
@@ -384,17 +305,14 @@ int petals_client_lm_head_backward(petals_client *client, void *dev_store, const
     const __half *E = (const __half *)c.p->embeddings, *x = (const __half *)hidden_in, *g = (const __half *)c.p->final_ln_g;
     __half *out = (__half *)grad_hidden_out;
     const float *part = (const float *)(store + p.part);
-    k_head_pack<<<dim3(p.sections, p.mtt), 1024, 0, st>>>(grad_logits, M, V, p.kt, p.sections, (__half *)(store + p.hi),
+    k_head_pack<<<dim3(p.sections, p.mtt), 64 * PACK_WAVES, 0, st>>>(grad_logits, M, V, p.kt, p.sections, (__half *)(store + p.hi),
                                                           p.pair ? (__half *)(store + p.lo) : nullptr, (float *)(store + p.unit));
     HIP_TRY(hipGetLastError());
-    if (p.pair) {
-        if (p.mt == 1) head_rows<1>(p, E, store, M, V, H, st);
-        else if (p.mt == 2) head_rows<2>(p, E, store, M, V, H, st);
-        else head_rows<4>(p, E, store, M, V, H, st);
-        HIP_TRY(hipGetLastError());
-    } else {
-        HIP_TRY(p.bm == 128 ? head_block<128>(p, E, store, M, V, H, st) : head_block<256>(p, E, store, M, V, H, st));
-    }
+    const hipError_t e = p.bm == 32    ? head_block<32, true>(p, E, store, M, V, H, st)
+                         : p.bm == 64  ? head_block<64, true>(p, E, store, M, V, H, st)
+                         : p.bm == 128 ? head_block<128, false>(p, E, store, M, V, H, st)
+                                       : head_block<256, false>(p, E, store, M, V, H, st);
+    HIP_TRY(e);
     if (H <= 2048) k_head_finish<256, 1><<<M, 256, 0, st>>>(part, p.splits, M, H, x, g, c.cfg->ln_eps, out);
     else if (H <= 4096) k_head_finish<512, 1><<<M, 512, 0, st>>>(part, p.splits, M, H, x, g, c.cfg->ln_eps, out);
     else if (H <= 8192) k_head_finish<1024, 1><<<M, 1024, 0, st>>>(part, p.splits, M, H, x, g, c.cfg->ln_eps, out);

@@ -99,3 +99,28 @@ __device__ __forceinline__ void ln_store(const float (&acc)[PER][8], __half *__r
         }
     }
 }
+// acc += rows 0 .. n - 1 in order, row(r) the address of row r; eight (fp32: four) of them on their way at once
+template <int NT, int PER, typename T, typename F>
+__device__ __forceinline__ void add_rows(float (&acc)[PER][8], int n, int H, F row) {
+    constexpr int AHEAD = sizeof(T) == 2 ? 8 : 4;
+    typedef T v8 __attribute__((ext_vector_type(8), aligned(2)));
+    for (int r0 = 0; r0 < n; r0 += AHEAD) {
+        const T *from[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; u++) from[u] = row(min(r0 + u, n - 1));
+#pragma unroll
+        for (int i = 0; i < PER; i++) {
+            const int k = (threadIdx.x + i * NT) * 8;
+            if (k >= H) continue;
+            v8 f[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; u++) f[u] = *(const v8 *)(from[u] + k);
+#pragma unroll
+            for (int u = 0; u < AHEAD; u++)
+                if (r0 + u < n) {
+#pragma unroll
+                    for (int e = 0; e < 8; e++) acc[i][e] += (float)f[u][e];
+                }
+        }
+    }
+}
