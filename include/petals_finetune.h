@@ -29,6 +29,7 @@ extern "C" {
 
 #define PETALS_LOGPROBS_TOP_MAX 64
 #define PETALS_DISTILL_TOP_MAX 1024
+#define PETALS_BACKWARD_ROWS_MAX (1 << 20)  /* rows of one of the two backward calls; above it PETALS_ERR_UNSUPPORTED */
 
 /*
  * Log probabilities of given tokens (scoring a text, or showing what a generation was sure of).

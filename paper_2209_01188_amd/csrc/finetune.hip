@@ -224,9 +224,10 @@ __global__ void __launch_bounds__(ROW_NT) k_logprobs(LogprobsOut o, int V, int r
 }
 
 // what the splits of a row have found
-constexpr int JOIN_NT = 1024, JOIN_NW = JOIN_NT / 64;
+template <int JOIN_NT>
 __global__ void __launch_bounds__(JOIN_NT) k_logprobs_join(LogprobsOut o, int V, int splits, double invT, int top_k,
                                                            const RowStat *__restrict__ stats, const uint64_t *__restrict__ tops) {
+    constexpr int JOIN_NW = JOIN_NT / 64;
     __shared__ RowStat sm[JOIN_NW];
     __shared__ uint64_t lists[JOIN_NW][64];
     const int t = blockIdx.x, n = splits * top_k;
@@ -510,21 +511,21 @@ __global__ void __launch_bounds__(1024) k_token_places(const int32_t *__restrict
 // How many pieces a list of n positions has, each of RUN_PIECE but the last, which takes what is left over as well
 __device__ __forceinline__ int run_pieces(int n) { return max(1, n / RUN_PIECE); }
 
-// number of different tokens before place p (over the workgroup); first is padded to 8 bytes
+// number of different tokens before place p, over the workgroup, in two parts with a barrier between them; first is padded to 8 bytes
 template <int NT>
-__device__ __forceinline__ int tokens_before(const uint8_t *__restrict__ first, int p, int *sm) {
+__device__ __forceinline__ void count_tokens(const uint8_t *__restrict__ first, int p, int *sm) {
     int n = 0;
     for (int q = threadIdx.x * 8; q < p; q += NT * 8) {
         const uint64_t w = *(const uint64_t *)(first + q);
         n += __popcll(p - q >= 8 ? w : w & ((1ull << (8 * (p - q))) - 1));
     }
     const float of_wave = wave_sum((float)n);                        // at most 2^24 of them
+    if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = (int)of_wave;
+}
+template <int NT>
+__device__ __forceinline__ int counted_tokens(const int *sm) {
     const int lane = threadIdx.x & 63;
-    if (lane == 0) sm[threadIdx.x >> 6] = (int)of_wave;
-    __syncthreads();
-    n = (int)wave_sum(lane < NT / 64 ? (float)sm[lane] : 0.0f);
-    __syncthreads();
-    return n;
+    return (int)wave_sum(lane < NT / 64 ? (float)sm[lane] : 0.0f);
 }
 
 // one workgroup per place: a place at which a piece of a token's list begins has work
@@ -539,21 +540,25 @@ __global__ void __launch_bounds__(NT) k_embed_backward(const __half *__restrict_
     const Place pl = places[p];
     const int piece = pl.before / RUN_PIECE, pieces = run_pieces(pl.count);
     if (p == M - 1) {
-        const int n = tokens_before<NT>(first, M, si);
+        count_tokens<NT>(first, M, si);
+        __syncthreads();
+        const int n = counted_tokens<NT>(si);
         if (threadIdx.x == 0) *count_out = n;
+        __syncthreads();
     }
     if (pl.before % RUN_PIECE || piece >= pieces) return;
     const int n = piece == pieces - 1 ? pl.count - pl.before : RUN_PIECE;
     LnRow<PER> row;
     if (pieces == 1) ln_load<NT, PER>(row, E + (size_t)pl.token * H, g, H);
-    const int u = pieces == 1 ? tokens_before<NT>(first, p, si) : 0;
     float acc[PER][8] = {};
     add_rows<NT, PER, _Float16>(acc, n, H, [&](int r) { return (const _Float16 *)grad + (size_t)places[p + r].position * H; });
     if (pieces > 1) {                                                // pieces begin at least RUN_PIECE places apart
         ln_store<NT, PER>(acc, parts + (size_t)(p / RUN_PIECE) * H, H);
         return;
     }
+    count_tokens<NT>(first, p, si);
     ln_backward<NT, PER>(acc, row, H, eps, sd);
+    const int u = counted_tokens<NT>(si);
     ln_store<NT, PER>(acc, grads_out + (size_t)u * H, H);
     if (threadIdx.x == 0) tokens_out[u] = pl.token;
 }
@@ -578,10 +583,11 @@ __global__ void __launch_bounds__(NT) k_embed_backward_join(int M, int H, const 
     const Place pl = places[p];
     LnRow<PER> row;
     ln_load<NT, PER>(row, E + (size_t)pl.token * H, g, H);
-    const int u = tokens_before<NT>(first, p, si);
     float acc[PER][8] = {};
     add_rows<NT, PER, float>(acc, run_pieces(pl.count), H, [&](int r) { return parts + (size_t)(p / RUN_PIECE + r) * H; });
+    count_tokens<NT>(first, p, si);
     ln_backward<NT, PER>(acc, row, H, eps, sd);
+    const int u = counted_tokens<NT>(si);
     ln_store<NT, PER>(acc, grads_out + (size_t)u * H, H);
     if (threadIdx.x == 0) tokens_out[u] = pl.token;
 }
@@ -638,7 +644,8 @@ int petals_client_logprobs(petals_client *client, const float *logits, const int
         k_logprobs<<<dim3(sp.splits, rows), ROW_NT, 0, st>>>(r, V, sp.range, invT, top_k, stats, tops);
         HIP_TRY(hipGetLastError());
         if (sp.splits > 1) {
-            k_logprobs_join<<<rows, JOIN_NT, 0, st>>>(r, V, sp.splits, invT, top_k, stats, tops);
+            if (sp.splits * top_k <= 1024) k_logprobs_join<256><<<rows, 256, 0, st>>>(r, V, sp.splits, invT, top_k, stats, tops);
+            else k_logprobs_join<1024><<<rows, 1024, 0, st>>>(r, V, sp.splits, invT, top_k, stats, tops);
             HIP_TRY(hipGetLastError());
         }
     }
@@ -679,6 +686,7 @@ int petals_client_embed_backward(petals_client *client, const int32_t *token_ids
     if (!client || !token_ids || !grad_hidden || !tokens_out || !grads_out || !count_out) return ps_fail(PETALS_ERR_INVALID_ARG, "null pointer");
     const ps_client_view c = ps_view(client);
     if (int rc = check_call(*c.cfg, M)) return rc;
+    if (M > PETALS_BACKWARD_ROWS_MAX) return ps_fail(PETALS_ERR_UNSUPPORTED, "%d rows exceed %d", M, PETALS_BACKWARD_ROWS_MAX);
     if (token_ids == tokens_out) return ps_fail(PETALS_ERR_INVALID_ARG, "token_ids and tokens_out alias");
     const int V = c.cfg->vocab, H = c.cfg->hidden;
     // M places of 16 bytes and their flags, then a row of partial sums for every RUN_PIECE places: some 17 M + (M / 32 + 1) 4 H bytes

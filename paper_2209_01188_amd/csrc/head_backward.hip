@@ -12,8 +12,6 @@
 
 namespace {
 
-constexpr int SECTION = 4096;              // columns of G that share a row's scale
-constexpr int SECTION_KT = SECTION / 32;   // in k-tiles
 typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));     // rows of an odd vocabulary begin anywhere
 
 // G as fp16 in the operand order of v_mfma_f32_16x16x32_f16: tile (mt, kt) of 16 rows x 32 columns is 1 KB, lane slot
@@ -22,7 +20,8 @@ typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));     // ro
 // mostly the label's, exactly.  lo (may be null): what the rounding left, in the same scale.
 // One workgroup per 16 rows and section; a wave reads PACK_TILES of its tiles, whole lines of 128 bytes, and stores them as they
 // are laid out.
-constexpr int PACK_WAVES = 16, PACK_TILES = SECTION_KT / PACK_WAVES;
+constexpr int PACK_TILES = 8;
+template <int PACK_WAVES>
 __global__ void __launch_bounds__(64 * PACK_WAVES) k_head_pack(const float *__restrict__ G, int M, int V, int KT, int sections,
                                                                __half *__restrict__ hi, __half *__restrict__ lo, float *__restrict__ unit) {
     __shared__ float most[16][PACK_WAVES];
@@ -32,7 +31,7 @@ __global__ void __launch_bounds__(64 * PACK_WAVES) k_head_pack(const float *__re
     float mx = 0.0f;
 #pragma unroll
     for (int i = 0; i < PACK_TILES; i++) {
-        const int kt = sec * SECTION_KT + wave * PACK_TILES + i, v = kt * 32 + (lane >> 4) * 8;
+        const int kt = (sec * PACK_WAVES + wave) * PACK_TILES + i, v = kt * 32 + (lane >> 4) * 8;
         if (kt * 32 + 32 <= V) {
             const v4f a = __builtin_nontemporal_load((const v4f_any *)(row + v)), b = __builtin_nontemporal_load((const v4f_any *)(row + v + 4));
 #pragma unroll
@@ -61,7 +60,7 @@ __global__ void __launch_bounds__(64 * PACK_WAVES) k_head_pack(const float *__re
     if (threadIdx.x < 16) unit[(size_t)t * sections + sec] = u;
 #pragma unroll
     for (int i = 0; i < PACK_TILES; i++) {
-        const int kt = sec * SECTION_KT + wave * PACK_TILES + i;
+        const int kt = (sec * PACK_WAVES + wave) * PACK_TILES + i;
         if (kt >= KT) break;
         v8h h, l;
 #pragma unroll
@@ -77,17 +76,19 @@ __global__ void __launch_bounds__(64 * PACK_WAVES) k_head_pack(const float *__re
 }
 
 // The product: output blocks of BM tokens x 256 columns, 8 waves of BM / 2 x 64, the contraction over the vocabulary split over
-// workgroups until every compute unit has one.  Token tiles and 32 rows x 512 bytes of E are copied to a ring of 4 slots in LDS,
-// three stages ahead.  The contraction runs along E's columns in memory, so its operands are turned around: a lane reads 4 columns
+// workgroups until every compute unit has one.  Token tiles and 32 rows x 512 bytes of E are copied to a ring of slots in LDS,
+// as many stages ahead as fit.  The contraction runs along E's columns in memory, so its operands are turned around: a lane reads 4 columns
 // of 8 rows and makes of them, one byte permutation per word, the A operands of 4 products (product i has columns 4 a + i).
 // PAIR: the token tiles twice, G's values and what their rounding left; calls of up to 64 rows, which wait for E's bytes anyway.
+constexpr int NSLOT = 4;
 template <int BM, bool PAIR>
 __global__ void __launch_bounds__(512, 2) k_head_block(const __half *__restrict__ E, const __half *__restrict__ hi, const __half *__restrict__ lo,
                                                        const float *__restrict__ unit, int M, int V, int H, int KT, int sections, int nb_m,
-                                                       int nb_n, int kt_per, float *__restrict__ part) {
+                                                       int nb_n, int kt_per, int section_kt, float *__restrict__ part) {
     constexpr int BN = 256, TM = BM / 32, TN = 4;               // tiles of 16 per wave: tokens, columns
-    constexpr int GT = BM / 16, GS = PAIR ? 8 : GT, SLOT = 16384 + GS * 1024, GL = GS / 8, LOADS = 2 + GL;
-    static_assert(GS % 8 == 0 && (!PAIR || 2 * GT <= 8), "as many token tiles to copy for every wave");
+    constexpr int GT = BM / 16, GS = PAIR ? 8 : GT, SLOT = 16384 + GS * 1024, GL = (GS + 7) / 8, LOADS = 2 + GL;
+    constexpr int FULL = GS % 8 ? GS % 8 : 8;                   // waves that copy GL token tiles per stage, the others one less
+    static_assert(!PAIR || 2 * GT <= 8, "a token tile for every wave");
     extern __shared__ __align__(16) unsigned char lds[];
     // workgroup -> block: an XCD (every eighth workgroup) takes a run of blocks of one split, four along the tokens at a time.
     // (Divisions are done by the vector unit; what is worked out from them is to be scalar all the same.)
@@ -98,9 +99,10 @@ __global__ void __launch_bounds__(512, 2) k_head_block(const __half *__restrict_
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 1, wn = wave >> 1;
     const int k0 = split * kt_per, k1 = min(KT, k0 + kt_per), MTT = (M + 15) >> 4;
 
-    // what this wave copies per stage: rows 4 wave .. + 4 of E, two per instruction, and GL token tiles.  (The buffer form: rows
-    // behind the matrix come as zeros.)
-    const uint32_t e_off = ((uint32_t)((wave * 4 + (lane >> 5)) * H) + (uint32_t)min(bn * BN + (lane & 31) * 8, H - 8)) * 2;
+    // what this wave copies per stage: rows 4 wave .. + 4 of E, two per instruction, and GL token tiles (fewer than 8 tiles of a
+    // pair: some waves copy one that nobody reads).  The buffer form: rows behind the matrix come as zeros.  The 128-byte halves
+    // of a row's 256 change places in every other octet of rows, so that the octets that are read together lie in different banks.
+    const uint32_t e_off = ((uint32_t)((wave * 4 + (lane >> 5)) * H) + (uint32_t)min(bn * BN + ((lane & 31) ^ (8 * ((wave >> 1) & 1))) * 8, H - 8)) * 2;
     const auto copy = [&](const void *base, uint32_t bytes, uint32_t off, int at) {
         __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)bytes, 0x00020000),
                                                  (__attribute__((address_space(3))) void *)(lds + at), 16, (int)off, 0, 0, 0);
@@ -110,15 +112,15 @@ __global__ void __launch_bounds__(512, 2) k_head_block(const __half *__restrict_
 #pragma unroll
         for (int i = 0; i < 2; i++) copy(E + (size_t)v * H, (uint32_t)rows * H * 2, e_off + i * 4u * H, slot * SLOT + (wave * 4 + 2 * i) * 512);
 #pragma unroll
-        for (int i = 0; i < GL; i++)
-        {   // (fewer than 8 tiles of a pair: some waves copy one that nobody reads)
-            const int tile = wave * GL + i;
+        for (int i = 0; i < GL; i++) {
+            const int tile = wave + 8 * i;
+            if (FULL < 8 && i == GL - 1 && wave >= FULL) break;
             copy((PAIR && tile >= GT ? lo : hi) + ((size_t)min(bm * GT + (PAIR ? tile % GT : tile), MTT - 1) * KT + k) * 512, 1024, lane * 16,
                  slot * SLOT + 16384 + tile * 1024);
         }
     };
     // operands: row 8 (lane / 16) + i, columns 64 wn + 4 (lane % 16) .. + 4; token tile j
-    const int e_at = (lane >> 4) * 8 * 512 + wn * 128 + (lane & 15) * 8, g_at = 16384 + wm * TM * 1024 + lane * 16;
+    const int e_at = (lane >> 4) * 8 * 512 + ((wn * 128 + (lane & 15) * 8) ^ (128 * ((lane >> 4) & 1))), g_at = 16384 + wm * TM * 1024 + lane * 16;
     const auto read_e = [&](int slot, int i) { return *(const v2i *)(lds + slot * SLOT + e_at + i * 512); };
     const auto read_g = [&](int slot, int j) { return *(const v8h *)(lds + slot * SLOT + g_at + (j < TM ? j : GT + j - TM) * 1024); };
 
@@ -127,35 +129,37 @@ __global__ void __launch_bounds__(512, 2) k_head_block(const __half *__restrict_
     for (int i = 0; i < TN; i++)
 #pragma unroll
         for (int j = 0; j < TM; j++) acc[i][j] = v4f{0, 0, 0, 0};
-    float u[TM];
     const uint32_t u_off = (lane & 15) * sections;
-    const auto unit_of = [&](int j, int kt) { return (unit + ((size_t)min(bm * GT + wm * TM + j, MTT - 1) * 16 * sections + kt / SECTION_KT))[u_off]; };
+    const auto unit_of = [&](int j, int kt) { return (unit + ((size_t)min(bm * GT + wm * TM + j, MTT - 1) * 16 * sections + kt / section_kt))[u_off]; };
 #pragma unroll
-    for (int j = 0; j < TM; j++) u[j] = unit_of(j, k0);
-
-#pragma unroll
-    for (int s = 0; s < 4; s++) copies(k0 + s, s);
+    for (int s = 0; s < NSLOT; s++) copies(k0 + s, s);
     v2i fe[2][8];
     constexpr int NG = PAIR ? 2 * TM : TM;
     v8h fg[2][NG];
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * LOADS) : "memory");
+    // at most `behind` stages' copies of this wave still on their way, its LDS reads done
+    const auto wait = [&](auto BEHIND) {
+        constexpr int behind = decltype(BEHIND)::value;
+        if (FULL < 8 && wave >= FULL) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(behind * (LOADS - 1)) : "memory");
+        else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(behind * LOADS) : "memory");
+    };
+    wait(std::integral_constant<int, NSLOT - 1>());
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 #pragma unroll
     for (int i = 0; i < 8; i++) fe[0][i] = read_e(0, i);
 #pragma unroll
     for (int j = 0; j < NG; j++) fg[0][j] = read_g(0, j);
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * LOADS) : "memory");
+    wait(std::integral_constant<int, NSLOT - 2>());
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 
-    // Stage kt: its operands are in registers, everybody has read slot kt % 4, and everybody's copies for stage kt + 1 have
-    // landed.  Beside the products, the copies of kt + 4 are requested and the operands of kt + 1 read, a few at a time.
+    // Stage kt: its operands are in registers, everybody has read its slot, and everybody's copies for stage kt + 1 have
+    // landed.  Beside the products, the copies of stage kt + NSLOT are requested and the operands of kt + 1 read, a few at a time.
     const auto stage = [&](int kt, auto S) {
-        constexpr int s = decltype(S)::value, cur = s & 1, nxt = cur ^ 1, next_slot = (s + 1) & 3;
+        constexpr int free_slot = decltype(S)::value, next_slot = (free_slot + 1) % NSLOT, cur = free_slot & 1, nxt = cur ^ 1;
         const auto beside = [&](int at) {                        // after eighth `at` of the products
             __builtin_amdgcn_sched_barrier(0);
-            if (at == 0) copies(kt + 4, s);
+            if (at == 0) copies(kt + NSLOT, free_slot);
             if (at == 1 || at == 2) {
 #pragma unroll
                 for (int r = 0; r < 4; r++) fe[nxt][4 * (at - 1) + r] = read_e(next_slot, 4 * (at - 1) + r);
@@ -181,18 +185,17 @@ __global__ void __launch_bounds__(512, 2) k_head_block(const __half *__restrict_
                 if (j == TM - 1) beside(2 * i + 1);
             }
         }
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * LOADS) : "memory");
+        wait(std::integral_constant<int, NSLOT - 2>());
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
     for (int kt = k0; kt < k1; kt += 4) {
-        if (kt % SECTION_KT == 0 && kt > k0) {                   // the next section has its own unit
+        if (!(kt & (section_kt - 1)) && kt > k0) {                   // the next section has its own unit
 #pragma unroll
             for (int j = 0; j < TM; j++) {
-                const float next = unit_of(j, kt), ratio = u[j] / next;
+                const float ratio = unit_of(j, kt - 1) / unit_of(j, kt);
 #pragma unroll
                 for (int i = 0; i < TN; i++) acc[i][j] *= ratio;
-                u[j] = next;
             }
         }
         stage(kt, std::integral_constant<int, 0>());
@@ -206,11 +209,12 @@ __global__ void __launch_bounds__(512, 2) k_head_block(const __half *__restrict_
     for (int j = 0; j < TM; j++) {
         const int t = (bm * GT + wm * TM + j) * 16 + (lane & 15);
         if (t >= M) continue;
+        const float u = unit_of(j, k1 - 1);
         float *o = part + ((size_t)split * M + t) * H;
 #pragma unroll
         for (int r = 0; r < 4; r++) {
             const int c = bn * BN + wn * 64 + (lane >> 4) * 16 + r * 4;
-            if (c < H) *(v4f *)(o + c) = v4f{acc[0][j][r], acc[1][j][r], acc[2][j][r], acc[3][j][r]} * u[j];
+            if (c < H) *(v4f *)(o + c) = v4f{acc[0][j][r], acc[1][j][r], acc[2][j][r], acc[3][j][r]} * u;
         }
     }
 }
@@ -224,31 +228,64 @@ __global__ void __launch_bounds__(NT) k_head_finish(const float *__restrict__ pa
     LnRow<PER> lr;
     ln_load<NT, PER>(lr, x + (size_t)t * H, g, H);
     float acc[PER][8] = {};
-    add_rows<NT, PER, float>(acc, splits, H, [&](int s) { return part + ((size_t)s * M + t) * H; });
+    add_rows<NT, PER, float, 8 / PER>(acc, splits, H, [&](int s) { return part + ((size_t)s * M + t) * H; });
     ln_backward<NT, PER>(acc, lr, H, eps, sm);
     ln_store<NT, PER>(acc, out + (size_t)t * H, H);
 }
 
 // How a call of M rows is cut up, and where things lie in its store
 struct HeadPlan {
-    int mtt, kt, sections;           // token tiles, k-tiles (a multiple of 4), sections of a row
+    int mtt, kt, section_kt, sections;   // token tiles, k-tiles (a multiple of 4), k-tiles of a section, sections of a row
     bool pair;
     int bm, nb_m, nb_n;              // tokens of a block, blocks
     int kt_per, splits;
     size_t hi, lo, unit, part, bytes;
 };
 HeadPlan head_plan(const petals_client_config &cfg, int M) {
+    constexpr int UNITS = 256;       // compute units: one workgroup each
     HeadPlan p;
     p.mtt = (M + 15) / 16;
     p.kt = (cfg.vocab + 127) / 128 * 4;
-    p.sections = (cfg.vocab + SECTION - 1) / SECTION;
+    // sections of 1024, 2048 or 4096 columns: a large call's products pay 1 % for the change of unit every 4096, a small call's
+    // packing takes the workgroups
+    p.section_kt = M <= 64 ? 32 : M <= 512 ? 64 : 128;
+    p.sections = (p.kt + p.section_kt - 1) / p.section_kt;
     p.pair = M <= PETALS_HEAD_BACKWARD_PAIR_ROWS;
-    p.bm = M <= 32 ? 32 : M <= 64 ? 64 : (M + 127) / 128 * 128 < (M + 255) / 256 * 256 ? 128 : 256;
-    p.nb_m = (M + p.bm - 1) / p.bm;
     p.nb_n = (cfg.hidden + 255) / 256;
-    const int want = max(1, 256 / (p.nb_m * p.nb_n));
-    p.kt_per = max(4, (p.kt / 4 + want - 1) / want * 4);
-    p.splits = (p.kt + p.kt_per - 1) / p.kt_per;
+    // Tokens of a block and splits of the contraction: the fewest stages one after the other, each at what it was measured to
+    // take (ns; 351 rows x 50257 x 2560 and 768 x 100003 x 4096), and the partial sums written and read.
+    const int shapes[3][2] = {{128, 520}, {192, 750}, {256, 860}}, one[1][2] = {{M <= 32 ? 32 : 64, 500}};
+    const int(*shape)[2] = p.pair ? one : shapes;
+    double best = 0.0;
+    for (int i = 0; i < (p.pair ? 1 : 3); i++) {
+        const int nb_m = (M + shape[i][0] - 1) / shape[i][0], blocks = nb_m * p.nb_n;
+        int before = 0;
+        for (int rounds = 1; rounds <= 8; rounds++) {
+            const int want = min((long long)UNITS * rounds / blocks, (long long)p.kt / 4);
+            if (want <= before) continue;
+            before = want;
+            const int kt_per = (p.kt / 4 + want - 1) / want * 4, splits = (p.kt + kt_per - 1) / kt_per;
+            const double ns = (double)(((long long)blocks * splits + UNITS - 1) / UNITS) * kt_per * shape[i][1] + splits * (double)M * cfg.hidden / 1200.0;
+            if (best == 0.0 || ns < best) {
+                best = ns;
+                p.bm = shape[i][0];
+                p.nb_m = nb_m;
+                p.kt_per = kt_per;
+                p.splits = splits;
+            }
+            if (p.pair) break;
+        }
+        if (!before) {                // more blocks than eight rounds hold
+            const double ns = (double)((blocks + UNITS - 1) / UNITS) * p.kt * shape[i][1] + (double)M * cfg.hidden / 1200.0;
+            if (best == 0.0 || ns < best) {
+                best = ns;
+                p.bm = shape[i][0];
+                p.nb_m = nb_m;
+                p.kt_per = p.kt;
+                p.splits = 1;
+            }
+        }
+    }
     const size_t tiles = ps_align_up((size_t)p.mtt * p.kt * 1024);
     p.hi = 0;
     p.lo = tiles;
@@ -260,7 +297,7 @@ HeadPlan head_plan(const petals_client_config &cfg, int M) {
 
 template <int BM, bool PAIR>
 hipError_t head_block(const HeadPlan &p, const __half *E, uint8_t *store, int M, int V, int H, hipStream_t st) {
-    constexpr int bytes = 4 * (16384 + (PAIR ? 8 : BM / 16) * 1024);
+    constexpr int bytes = NSLOT * (16384 + (PAIR ? 8 : BM / 16) * 1024);
     {   // the limit belongs to the function, for the whole process
         static std::mutex attr_lock;
         static bool attr_set = false;
@@ -272,7 +309,7 @@ hipError_t head_block(const HeadPlan &p, const __half *E, uint8_t *store, int M,
     }
     k_head_block<BM, PAIR><<<p.nb_m * p.nb_n * p.splits, 512, bytes, st>>>(E, (const __half *)(store + p.hi), (const __half *)(store + p.lo),
                                                                           (const float *)(store + p.unit), M, V, H, p.kt, p.sections, p.nb_m,
-                                                                          p.nb_n, p.kt_per, (float *)(store + p.part));
+                                                                          p.nb_n, p.kt_per, p.section_kt, (float *)(store + p.part));
     return hipGetLastError();
 }
 
@@ -285,6 +322,7 @@ int petals_client_lm_head_backward_bytes(const petals_client_config *cfg, int32_
     if (int rc = ps_check_client_config(cfg)) return rc;
     if (M < 1) return ps_fail(PETALS_ERR_INVALID_ARG, "M must be positive");
     if (M > cfg->max_rows_per_call) return ps_fail(PETALS_ERR_CAPACITY, "%d rows exceed max_rows_per_call %d", M, cfg->max_rows_per_call);
+    if (M > PETALS_BACKWARD_ROWS_MAX) return ps_fail(PETALS_ERR_UNSUPPORTED, "%d rows exceed %d", M, PETALS_BACKWARD_ROWS_MAX);
     *bytes = head_plan(*cfg, M).bytes;
     return PETALS_OK;
 }
@@ -296,6 +334,7 @@ int petals_client_lm_head_backward(petals_client *client, void *dev_store, const
     const ps_client_view c = ps_view(client);
     if (M < 1) return ps_fail(PETALS_ERR_INVALID_ARG, "M must be positive");
     if (M > c.cfg->max_rows_per_call) return ps_fail(PETALS_ERR_CAPACITY, "%d rows exceed max_rows_per_call %d", M, c.cfg->max_rows_per_call);
+    if (M > PETALS_BACKWARD_ROWS_MAX) return ps_fail(PETALS_ERR_UNSUPPORTED, "%d rows exceed %d", M, PETALS_BACKWARD_ROWS_MAX);
     if (grad_hidden_out == hidden_in || grad_hidden_out == (const void *)grad_logits)
         return ps_fail(PETALS_ERR_INVALID_ARG, "buffers alias");
     const HeadPlan p = head_plan(*c.cfg, M);
@@ -305,12 +344,14 @@ int petals_client_lm_head_backward(petals_client *client, void *dev_store, const
     const __half *E = (const __half *)c.p->embeddings, *x = (const __half *)hidden_in, *g = (const __half *)c.p->final_ln_g;
     __half *out = (__half *)grad_hidden_out;
     const float *part = (const float *)(store + p.part);
-    k_head_pack<<<dim3(p.sections, p.mtt), 64 * PACK_WAVES, 0, st>>>(grad_logits, M, V, p.kt, p.sections, (__half *)(store + p.hi),
-                                                          p.pair ? (__half *)(store + p.lo) : nullptr, (float *)(store + p.unit));
+    const auto pack = p.section_kt == 32 ? k_head_pack<4> : p.section_kt == 64 ? k_head_pack<8> : k_head_pack<16>;
+    pack<<<dim3(p.sections, p.mtt), 64 * (p.section_kt / PACK_TILES), 0, st>>>(grad_logits, M, V, p.kt, p.sections, (__half *)(store + p.hi),
+                                                                               p.pair ? (__half *)(store + p.lo) : nullptr, (float *)(store + p.unit));
     HIP_TRY(hipGetLastError());
     const hipError_t e = p.bm == 32    ? head_block<32, true>(p, E, store, M, V, H, st)
                          : p.bm == 64  ? head_block<64, true>(p, E, store, M, V, H, st)
                          : p.bm == 128 ? head_block<128, false>(p, E, store, M, V, H, st)
+                         : p.bm == 192 ? head_block<192, false>(p, E, store, M, V, H, st)
                                        : head_block<256, false>(p, E, store, M, V, H, st);
     HIP_TRY(e);
     if (H <= 2048) k_head_finish<256, 1><<<M, 256, 0, st>>>(part, p.splits, M, H, x, g, c.cfg->ln_eps, out);

@@ -1,5 +1,6 @@
 // Derivative of a LayerNorm y = g x_hat + b, x_hat = (x - mean) / sqrt(var + eps), of one row by one workgroup:
 //   dx = inv (dy g - mean(dy g) - x_hat mean(dy g x_hat)),  inv = 1 / sqrt(var + eps)
+// (Its barriers order LDS only.)
 // All row sums in fp64, the variance about the mean.
 #pragma once
 #include "common.h"
@@ -41,11 +42,11 @@ __device__ __forceinline__ void ln_backward(float (&acc)[PER][8], const LnRow<PE
             sm[threadIdx.x >> 6][0] = a;
             sm[threadIdx.x >> 6][1] = b;
         }
-        __syncthreads();
+        lds_barrier();
         const int lane = threadIdx.x & 63;                          // (all waves' sums in one lane would be 4 registers each)
         a = wave_sum(lane < NT / 64 ? sm[lane][0] : 0.0);
         b = wave_sum(lane < NT / 64 ? sm[lane][1] : 0.0);
-        __syncthreads();
+        lds_barrier();
     };
     both(s1, sa);
     const double rH = 1.0 / (double)H, mean = s1 * rH, ma = sa * rH;
@@ -99,10 +100,9 @@ __device__ __forceinline__ void ln_store(const float (&acc)[PER][8], __half *__r
         }
     }
 }
-// acc += rows 0 .. n - 1 in order, row(r) the address of row r; eight (fp32: four) of them on their way at once
-template <int NT, int PER, typename T, typename F>
+// acc += rows 0 .. n - 1 in order, row(r) the address of row r; AHEAD of them on their way at once
+template <int NT, int PER, typename T, int AHEAD = sizeof(T) == 2 ? 8 : 4, typename F>
 __device__ __forceinline__ void add_rows(float (&acc)[PER][8], int n, int H, F row) {
-    constexpr int AHEAD = sizeof(T) == 2 ? 8 : 4;
     typedef T v8 __attribute__((ext_vector_type(8), aligned(2)));
     for (int r0 = 0; r0 < n; r0 += AHEAD) {
         const T *from[AHEAD];
