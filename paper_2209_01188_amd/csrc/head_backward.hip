@@ -10,6 +10,9 @@
 #include "ln_backward.h"
 #include "span_internal.h"
 
+#ifndef SBIG
+#define SBIG 64
+#endif
 namespace {
 
 typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));     // rows of an odd vocabulary begin anywhere
@@ -18,60 +21,62 @@ typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));     // ro
 // 16 (column / 8) + row holds 8 columns.  A row's section is scaled so that its largest value becomes 32768: fp16 then keeps
 // 2^-12 of a value down to 2^-29 of the largest (a softmax's gradient reaches from 1 down to 1e-9 and less), and the largest,
 // mostly the label's, exactly.  lo (may be null): what the rounding left, in the same scale.
-// One workgroup per 16 rows and section; a wave reads PACK_TILES of its tiles, whole lines of 128 bytes, and stores them as they
-// are laid out.
-constexpr int PACK_TILES = 8;
-template <int PACK_WAVES>
-__global__ void __launch_bounds__(64 * PACK_WAVES) k_head_pack(const float *__restrict__ G, int M, int V, int KT, int sections,
-                                                               __half *__restrict__ hi, __half *__restrict__ lo, float *__restrict__ unit) {
-    __shared__ float most[16][PACK_WAVES];
-    const int sec = blockIdx.x, mt = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, t = mt * 16 + r;
+// A wave per row and section, SKT k-tiles: it reads 1 KB of the row at a time (a row of an odd vocabulary begins anywhere; the
+// tiles' own 128 bytes of it would touch two lines each), takes the maximum, and drops its halves into LDS where the tiles lie;
+// from there they go out as whole tiles of 16 rows.  272 bytes from one group of 8 columns to the next, so that the 64 lanes'
+// halves fall on different banks.
+constexpr int PACK_GROUP = 16 * 16 + 16, PACK_TILE = 4 * PACK_GROUP;
+template <int SKT, bool PAIR>
+__global__ void __launch_bounds__(1024) k_head_pack(const float *__restrict__ G, int M, int V, int KT, int sections,
+                                                    __half *__restrict__ hi, __half *__restrict__ lo, float *__restrict__ unit) {
+    extern __shared__ __align__(16) unsigned char lds[];
+    constexpr int STEPS = SKT / 8;
+    const int sec = blockIdx.x, mt = blockIdx.y, lane = threadIdx.x & 63, r = threadIdx.x >> 6, t = mt * 16 + r, v0 = sec * SKT * 32 + lane * 4;
     const float *row = G + (size_t)min(t, M - 1) * V;
-    float f[PACK_TILES][8];
+    float f[STEPS][4];
     float mx = 0.0f;
 #pragma unroll
-    for (int i = 0; i < PACK_TILES; i++) {
-        const int kt = (sec * PACK_WAVES + wave) * PACK_TILES + i, v = kt * 32 + (lane >> 4) * 8;
-        if (kt * 32 + 32 <= V) {
-            const v4f a = __builtin_nontemporal_load((const v4f_any *)(row + v)), b = __builtin_nontemporal_load((const v4f_any *)(row + v + 4));
+    for (int i = 0; i < STEPS; i++) {
+        const int v = v0 + i * 256;
+        if (v + 3 < V) {
+            const v4f a = __builtin_nontemporal_load((const v4f_any *)(row + v));
 #pragma unroll
-            for (int e = 0; e < 4; e++) {
-                f[i][e] = a[e];
-                f[i][4 + e] = b[e];
-            }
+            for (int e = 0; e < 4; e++) f[i][e] = a[e];
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; e++) f[i][e] = v + e < V ? row[v + e] : 0.0f;
+            for (int e = 0; e < 4; e++) f[i][e] = v + e < V ? row[v + e] : 0.0f;
         }
     }
 #pragma unroll
-    for (int i = 0; i < PACK_TILES; i++)
+    for (int i = 0; i < STEPS; i++)
 #pragma unroll
-        for (int e = 0; e < 8; e++) mx = fmaxf(mx, fabsf(f[i][e]));
-    mx = fmaxf(mx, __shfl_xor(mx, 16));
-    mx = fmaxf(mx, __shfl_xor(mx, 32));
-    if (lane < 16) most[r][wave] = mx;
-    __syncthreads();
-    mx = 0.0f;
-#pragma unroll
-    for (int w = 0; w < PACK_WAVES; w++) mx = fmaxf(mx, most[r][w]);
+        for (int e = 0; e < 4; e++) mx = fmaxf(mx, fabsf(f[i][e]));
+    mx = wave_max(mx);
     // (rows behind the call's, sections of zeros and of next to nothing: a unit of 2^-60, so that the ratio of two units stays a number)
     const float u = t < M ? fmaxf(mx * 0x1p-15f, 0x1p-60f) : 0x1p-60f, s = t < M ? 1.0f / u : 0.0f;
-    if (threadIdx.x < 16) unit[(size_t)t * sections + sec] = u;
+    if (lane == 0) unit[(size_t)t * sections + sec] = u;
+    unsigned char *mine = lds + (lane >> 3) * PACK_TILE + ((lane & 7) >> 1) * PACK_GROUP + r * 16 + (lane & 1) * 8;
 #pragma unroll
-    for (int i = 0; i < PACK_TILES; i++) {
-        const int kt = (sec * PACK_WAVES + wave) * PACK_TILES + i;
-        if (kt >= KT) break;
-        v8h h, l;
+    for (int i = 0; i < STEPS; i++) {
+        v4h h, l;
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
+        for (int e = 0; e < 4; e++) {
             const float x = f[i][e] * s;
             h[e] = (_Float16)x;
             l[e] = (_Float16)(x - (float)h[e]);
         }
-        const size_t at = (((size_t)mt * KT + kt) * 64 + lane) * 8;
-        *(v8h *)(hi + at) = h;
-        if (lo) *(v8h *)(lo + at) = l;
+        *(v4h *)(mine + i * 8 * PACK_TILE) = h;
+        if (PAIR) *(v4h *)(mine + (SKT + i * 8) * PACK_TILE) = l;
+    }
+    __syncthreads();
+    const int at = (lane >> 4) * PACK_GROUP + (lane & 15) * 16;
+#pragma unroll
+    for (int i = r; i < SKT; i += 16) {
+        const int kt = sec * SKT + i;
+        if (kt >= KT) break;
+        const size_t to = (((size_t)mt * KT + kt) * 64 + lane) * 8;
+        *(v8h *)(hi + to) = *(const v8h *)(lds + i * PACK_TILE + at);
+        if (PAIR) *(v8h *)(lo + to) = *(const v8h *)(lds + (SKT + i) * PACK_TILE + at);
     }
 }
 
@@ -246,11 +251,11 @@ HeadPlan head_plan(const petals_client_config &cfg, int M) {
     HeadPlan p;
     p.mtt = (M + 15) / 16;
     p.kt = (cfg.vocab + 127) / 128 * 4;
+    p.pair = M <= PETALS_HEAD_BACKWARD_PAIR_ROWS;
     // sections of 1024, 2048 or 4096 columns: a large call's products pay 1 % for the change of unit every 4096, a small call's
     // packing takes the workgroups
-    p.section_kt = M <= 64 ? 32 : M <= 512 ? 64 : 128;
+    p.section_kt = p.pair ? 32 : M <= 512 ? 64 : SBIG;
     p.sections = (p.kt + p.section_kt - 1) / p.section_kt;
-    p.pair = M <= PETALS_HEAD_BACKWARD_PAIR_ROWS;
     p.nb_n = (cfg.hidden + 255) / 256;
     // Tokens of a block and splits of the contraction: the fewest stages one after the other, each at what it was measured to
     // take (ns; 351 rows x 50257 x 2560 and 768 x 100003 x 4096), and the partial sums written and read.
@@ -295,18 +300,33 @@ HeadPlan head_plan(const petals_client_config &cfg, int M) {
     return p;
 }
 
+// The limit of a kernel's dynamic LDS belongs to the function, for the whole process: set once
+struct LdsLimit {
+    std::mutex lock;
+    bool set = false;
+    hipError_t allow(const void *kernel, int bytes) {
+        std::lock_guard<std::mutex> hold(lock);
+        if (set) return hipSuccess;
+        const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        set = e == hipSuccess;
+        return e;
+    }
+};
+
+template <int SKT, bool PAIR>
+hipError_t head_pack(const HeadPlan &p, const float *G, uint8_t *store, int M, int V, hipStream_t st) {
+    constexpr int bytes = SKT * PACK_TILE * (PAIR ? 2 : 1);
+    static LdsLimit limit;
+    if (hipError_t e = limit.allow((const void *)k_head_pack<SKT, PAIR>, bytes)) return e;
+    k_head_pack<SKT, PAIR><<<dim3(p.sections, p.mtt), 1024, bytes, st>>>(G, M, V, p.kt, p.sections, (__half *)(store + p.hi), (__half *)(store + p.lo),
+                                                                        (float *)(store + p.unit));
+    return hipGetLastError();
+}
 template <int BM, bool PAIR>
 hipError_t head_block(const HeadPlan &p, const __half *E, uint8_t *store, int M, int V, int H, hipStream_t st) {
     constexpr int bytes = NSLOT * (16384 + (PAIR ? 8 : BM / 16) * 1024);
-    {   // the limit belongs to the function, for the whole process
-        static std::mutex attr_lock;
-        static bool attr_set = false;
-        std::lock_guard<std::mutex> hold(attr_lock);
-        if (!attr_set) {
-            if (hipError_t e = hipFuncSetAttribute((const void *)k_head_block<BM, PAIR>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes)) return e;
-            attr_set = true;
-        }
-    }
+    static LdsLimit limit;
+    if (hipError_t e = limit.allow((const void *)k_head_block<BM, PAIR>, bytes)) return e;
     k_head_block<BM, PAIR><<<p.nb_m * p.nb_n * p.splits, 512, bytes, st>>>(E, (const __half *)(store + p.hi), (const __half *)(store + p.lo),
                                                                           (const float *)(store + p.unit), M, V, H, p.kt, p.sections, p.nb_m,
                                                                           p.nb_n, p.kt_per, p.section_kt, (float *)(store + p.part));
@@ -344,15 +364,15 @@ int petals_client_lm_head_backward(petals_client *client, void *dev_store, const
     const __half *E = (const __half *)c.p->embeddings, *x = (const __half *)hidden_in, *g = (const __half *)c.p->final_ln_g;
     __half *out = (__half *)grad_hidden_out;
     const float *part = (const float *)(store + p.part);
-    const auto pack = p.section_kt == 32 ? k_head_pack<4> : p.section_kt == 64 ? k_head_pack<8> : k_head_pack<16>;
-    pack<<<dim3(p.sections, p.mtt), 64 * (p.section_kt / PACK_TILES), 0, st>>>(grad_logits, M, V, p.kt, p.sections, (__half *)(store + p.hi),
-                                                                               p.pair ? (__half *)(store + p.lo) : nullptr, (float *)(store + p.unit));
-    HIP_TRY(hipGetLastError());
-    const hipError_t e = p.bm == 32    ? head_block<32, true>(p, E, store, M, V, H, st)
-                         : p.bm == 64  ? head_block<64, true>(p, E, store, M, V, H, st)
-                         : p.bm == 128 ? head_block<128, false>(p, E, store, M, V, H, st)
-                         : p.bm == 192 ? head_block<192, false>(p, E, store, M, V, H, st)
-                                       : head_block<256, false>(p, E, store, M, V, H, st);
+    hipError_t e = p.section_kt == 32   ? head_pack<32, true>(p, grad_logits, store, M, V, st)
+                   : p.section_kt == 64 ? head_pack<64, false>(p, grad_logits, store, M, V, st)
+                                        : head_pack<128, false>(p, grad_logits, store, M, V, st);
+    HIP_TRY(e);
+    e = p.bm == 32    ? head_block<32, true>(p, E, store, M, V, H, st)
+        : p.bm == 64  ? head_block<64, true>(p, E, store, M, V, H, st)
+        : p.bm == 128 ? head_block<128, false>(p, E, store, M, V, H, st)
+        : p.bm == 192 ? head_block<192, false>(p, E, store, M, V, H, st)
+                      : head_block<256, false>(p, E, store, M, V, H, st);
     HIP_TRY(e);
     if (H <= 2048) k_head_finish<256, 1><<<M, 256, 0, st>>>(part, p.splits, M, H, x, g, c.cfg->ln_eps, out);
     else if (H <= 4096) k_head_finish<512, 1><<<M, 512, 0, st>>>(part, p.splits, M, H, x, g, c.cfg->ln_eps, out);
