@@ -10,9 +10,6 @@
 #include "ln_backward.h"
 #include "span_internal.h"
 
-#ifndef SBIG
-#define SBIG 64
-#endif
 namespace {
 
 typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));     // rows of an odd vocabulary begin anywhere
@@ -26,11 +23,12 @@ typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));     // ro
 // from there they go out as whole tiles of 16 rows.  272 bytes from one group of 8 columns to the next, so that the 64 lanes'
 // halves fall on different banks.
 constexpr int PACK_GROUP = 16 * 16 + 16, PACK_TILE = 4 * PACK_GROUP;
-template <int SKT, bool PAIR>
-__global__ void __launch_bounds__(1024) k_head_pack(const float *__restrict__ G, int M, int V, int KT, int sections,
+constexpr int head_section_kt(bool pair) { return pair ? 32 : 64; }
+template <bool PAIR>
+__global__ void __launch_bounds__(1024) k_head_pack(const float *__restrict__ G, int M, int V, int KT,
                                                     __half *__restrict__ hi, __half *__restrict__ lo, float *__restrict__ unit) {
     extern __shared__ __align__(16) unsigned char lds[];
-    constexpr int STEPS = SKT / 8;
+    constexpr int SKT = head_section_kt(PAIR), STEPS = SKT / 8;
     const int sec = blockIdx.x, mt = blockIdx.y, lane = threadIdx.x & 63, r = threadIdx.x >> 6, t = mt * 16 + r, v0 = sec * SKT * 32 + lane * 4;
     const float *row = G + (size_t)min(t, M - 1) * V;
     float f[STEPS][4];
@@ -54,7 +52,7 @@ __global__ void __launch_bounds__(1024) k_head_pack(const float *__restrict__ G,
     mx = wave_max(mx);
     // (rows behind the call's, sections of zeros and of next to nothing: a unit of 2^-60, so that the ratio of two units stays a number)
     const float u = t < M ? fmaxf(mx * 0x1p-15f, 0x1p-60f) : 0x1p-60f, s = t < M ? 1.0f / u : 0.0f;
-    if (lane == 0) unit[(size_t)t * sections + sec] = u;
+    if (lane == 0) unit[(size_t)sec * gridDim.y * 16 + t] = u;
     unsigned char *mine = lds + (lane >> 3) * PACK_TILE + ((lane & 7) >> 1) * PACK_GROUP + r * 16 + (lane & 1) * 8;
 #pragma unroll
     for (int i = 0; i < STEPS; i++) {
@@ -88,11 +86,12 @@ __global__ void __launch_bounds__(1024) k_head_pack(const float *__restrict__ G,
 constexpr int NSLOT = 4;
 template <int BM, bool PAIR>
 __global__ void __launch_bounds__(512, 2) k_head_block(const __half *__restrict__ E, const __half *__restrict__ hi, const __half *__restrict__ lo,
-                                                       const float *__restrict__ unit, int M, int V, int H, int KT, int sections, int nb_m,
-                                                       int nb_n, int kt_per, int section_kt, float *__restrict__ part) {
+                                                       const float *__restrict__ unit, int M, int V, int H, int KT, int nb_m,
+                                                       int nb_n, int kt_per, float *__restrict__ part) {
     constexpr int BN = 256, TM = BM / 32, TN = 4;               // tiles of 16 per wave: tokens, columns
     constexpr int GT = BM / 16, GS = PAIR ? 8 : GT, SLOT = 16384 + GS * 1024, GL = (GS + 7) / 8, LOADS = 2 + GL;
     constexpr int FULL = GS % 8 ? GS % 8 : 8;                   // waves that copy GL token tiles per stage, the others one less
+    constexpr int section_kt = head_section_kt(PAIR);
     static_assert(!PAIR || 2 * GT <= 8, "a token tile for every wave");
     extern __shared__ __align__(16) unsigned char lds[];
     // workgroup -> block: an XCD (every eighth workgroup) takes a run of blocks of one split, four along the tokens at a time.
@@ -134,8 +133,15 @@ __global__ void __launch_bounds__(512, 2) k_head_block(const __half *__restrict_
     for (int i = 0; i < TN; i++)
 #pragma unroll
         for (int j = 0; j < TM; j++) acc[i][j] = v4f{0, 0, 0, 0};
-    const uint32_t u_off = (lane & 15) * sections;
-    const auto unit_of = [&](int j, int kt) { return (unit + ((size_t)min(bm * GT + wm * TM + j, MTT - 1) * 16 * sections + kt / section_kt))[u_off]; };
+    // the units of a section's rows, two sections at a time in LDS behind the ring
+    const int rows = MTT * 16;
+    const auto copy_units = [&](int kt) {
+        const int sec = kt / section_kt;
+        if (wave == 0) copy(unit + (size_t)sec * rows, rows * 4, bm * BM * 4 + lane * 16, NSLOT * SLOT + (sec & 1) * 1024);
+    };
+    const auto unit_of = [&](int j, int kt) { return *(const float *)(lds + NSLOT * SLOT + ((kt / section_kt) & 1) * 1024 + ((wm * TM + j) * 16 + (lane & 15)) * 4); };
+    copy_units(k0);
+    copy_units(min(k0 + section_kt, KT - 1));
 #pragma unroll
     for (int s = 0; s < NSLOT; s++) copies(k0 + s, s);
     v2i fe[2][8];
@@ -198,10 +204,12 @@ __global__ void __launch_bounds__(512, 2) k_head_block(const __half *__restrict_
         if (!(kt & (section_kt - 1)) && kt > k0) {                   // the next section has its own unit
 #pragma unroll
             for (int j = 0; j < TM; j++) {
-                const float ratio = unit_of(j, kt - 1) / unit_of(j, kt);
+                const float ratio = unit_of(j, kt - section_kt) / unit_of(j, kt);
 #pragma unroll
                 for (int i = 0; i < TN; i++) acc[i][j] *= ratio;
             }
+            lds_barrier();                                       // everybody has read the section before: the one behind takes its place
+            copy_units(min(kt + section_kt, KT - 1));
         }
         stage(kt, std::integral_constant<int, 0>());
         stage(kt + 1, std::integral_constant<int, 1>());
@@ -214,7 +222,7 @@ __global__ void __launch_bounds__(512, 2) k_head_block(const __half *__restrict_
     for (int j = 0; j < TM; j++) {
         const int t = (bm * GT + wm * TM + j) * 16 + (lane & 15);
         if (t >= M) continue;
-        const float u = unit_of(j, k1 - 1);
+        const float u = unit[(size_t)((k1 - 1) / section_kt) * rows + t];
         float *o = part + ((size_t)split * M + t) * H;
 #pragma unroll
         for (int r = 0; r < 4; r++) {
@@ -240,7 +248,7 @@ __global__ void __launch_bounds__(NT) k_head_finish(const float *__restrict__ pa
 
 // How a call of M rows is cut up, and where things lie in its store
 struct HeadPlan {
-    int mtt, kt, section_kt, sections;   // token tiles, k-tiles (a multiple of 4), k-tiles of a section, sections of a row
+    int mtt, kt, sections;           // token tiles, k-tiles (a multiple of 4), sections of a row
     bool pair;
     int bm, nb_m, nb_n;              // tokens of a block, blocks
     int kt_per, splits;
@@ -252,10 +260,7 @@ HeadPlan head_plan(const petals_client_config &cfg, int M) {
     p.mtt = (M + 15) / 16;
     p.kt = (cfg.vocab + 127) / 128 * 4;
     p.pair = M <= PETALS_HEAD_BACKWARD_PAIR_ROWS;
-    // sections of 1024, 2048 or 4096 columns: a large call's products pay 1 % for the change of unit every 4096, a small call's
-    // packing takes the workgroups
-    p.section_kt = p.pair ? 32 : M <= 512 ? 64 : SBIG;
-    p.sections = (p.kt + p.section_kt - 1) / p.section_kt;
+    p.sections = (p.kt + head_section_kt(p.pair) - 1) / head_section_kt(p.pair);
     p.nb_n = (cfg.hidden + 255) / 256;
     // Tokens of a block and splits of the contraction: the fewest stages one after the other, each at what it was measured to
     // take (ns; 351 rows x 50257 x 2560 and 768 x 100003 x 4096), and the partial sums written and read.
@@ -313,23 +318,23 @@ struct LdsLimit {
     }
 };
 
-template <int SKT, bool PAIR>
+template <bool PAIR>
 hipError_t head_pack(const HeadPlan &p, const float *G, uint8_t *store, int M, int V, hipStream_t st) {
-    constexpr int bytes = SKT * PACK_TILE * (PAIR ? 2 : 1);
+    constexpr int bytes = head_section_kt(PAIR) * PACK_TILE * (PAIR ? 2 : 1);
     static LdsLimit limit;
-    if (hipError_t e = limit.allow((const void *)k_head_pack<SKT, PAIR>, bytes)) return e;
-    k_head_pack<SKT, PAIR><<<dim3(p.sections, p.mtt), 1024, bytes, st>>>(G, M, V, p.kt, p.sections, (__half *)(store + p.hi), (__half *)(store + p.lo),
+    if (hipError_t e = limit.allow((const void *)k_head_pack<PAIR>, bytes)) return e;
+    k_head_pack<PAIR><<<dim3(p.sections, p.mtt), 1024, bytes, st>>>(G, M, V, p.kt, (__half *)(store + p.hi), (__half *)(store + p.lo),
                                                                         (float *)(store + p.unit));
     return hipGetLastError();
 }
 template <int BM, bool PAIR>
 hipError_t head_block(const HeadPlan &p, const __half *E, uint8_t *store, int M, int V, int H, hipStream_t st) {
-    constexpr int bytes = NSLOT * (16384 + (PAIR ? 8 : BM / 16) * 1024);
+    constexpr int bytes = NSLOT * (16384 + (PAIR ? 8 : BM / 16) * 1024) + 2048;
     static LdsLimit limit;
     if (hipError_t e = limit.allow((const void *)k_head_block<BM, PAIR>, bytes)) return e;
     k_head_block<BM, PAIR><<<p.nb_m * p.nb_n * p.splits, 512, bytes, st>>>(E, (const __half *)(store + p.hi), (const __half *)(store + p.lo),
-                                                                          (const float *)(store + p.unit), M, V, H, p.kt, p.sections, p.nb_m,
-                                                                          p.nb_n, p.kt_per, p.section_kt, (float *)(store + p.part));
+                                                                          (const float *)(store + p.unit), M, V, H, p.kt, p.nb_m,
+                                                                          p.nb_n, p.kt_per, (float *)(store + p.part));
     return hipGetLastError();
 }
 
@@ -364,9 +369,7 @@ int petals_client_lm_head_backward(petals_client *client, void *dev_store, const
     const __half *E = (const __half *)c.p->embeddings, *x = (const __half *)hidden_in, *g = (const __half *)c.p->final_ln_g;
     __half *out = (__half *)grad_hidden_out;
     const float *part = (const float *)(store + p.part);
-    hipError_t e = p.section_kt == 32   ? head_pack<32, true>(p, grad_logits, store, M, V, st)
-                   : p.section_kt == 64 ? head_pack<64, false>(p, grad_logits, store, M, V, st)
-                                        : head_pack<128, false>(p, grad_logits, store, M, V, st);
+    hipError_t e = p.pair ? head_pack<true>(p, grad_logits, store, M, V, st) : head_pack<false>(p, grad_logits, store, M, V, st);
     HIP_TRY(e);
     e = p.bm == 32    ? head_block<32, true>(p, E, store, M, V, H, st)
         : p.bm == 64  ? head_block<64, true>(p, E, store, M, V, H, st)
