@@ -29,7 +29,7 @@ extern "C" {
 
 #define PETALS_LOGPROBS_TOP_MAX 64
 #define PETALS_DISTILL_TOP_MAX 1024
-#define PETALS_BACKWARD_ROWS_MAX (1 << 20)  /* rows of one of the two backward calls; above it PETALS_ERR_UNSUPPORTED */
+#define PETALS_BACKWARD_ROWS_MAX (1 << 20)  /* rows of one of the two backward calls (and 2^30 tokens of any vocabulary here): above it PETALS_ERR_UNSUPPORTED */
 
 /*
  * Log probabilities of given tokens (scoring a text, or showing what a generation was sure of).
@@ -39,7 +39,7 @@ extern "C" {
  *   top_out[t][i]       dev int32 [M, top_k]: the token with the i-th largest logit (equal logits: lower index first)
  *   top_logprob_out     dev fp32 [M, top_k]: its log probability
  * logits: dev fp32 [M, V]; tokens: dev int32 [M], may be NULL together with logprob_out; entropy_out may be NULL; with
- * top_k = 0 the last two are NULL.  temperature > 0 (not infinite); top_k <= min(V, PETALS_LOGPROBS_TOP_MAX), above
+ * top_k = 0 the last two are NULL.  temperature at least 1e-38 and not infinite; top_k <= min(V, PETALS_LOGPROBS_TOP_MAX), above
  * PETALS_LOGPROBS_TOP_MAX -> PETALS_ERR_UNSUPPORTED.  M <= max_rows_per_call, else PETALS_ERR_CAPACITY.  Sums are held
  * in fp64.  A row without a distribution: all log probabilities -infinity, entropy 0, tokens 0, 1, 2, ...
  */
@@ -63,7 +63,7 @@ int petals_client_logprobs(petals_client *client, const float *logits, const int
  *   grad_logits_out   dev fp32 [M, V], may be NULL if loss_out is given; may be the same memory as logits
  * A row without a list (no entry, or all teacher logits -infinity) has loss 0 and gradient 0.  A row without a distribution
  * of its own (and with a list) has loss +infinity and gradient 0.  1 <= K <= PETALS_DISTILL_TOP_MAX, above it
- * PETALS_ERR_UNSUPPORTED; temperature > 0 (not infinite); M <= max_rows_per_call, else PETALS_ERR_CAPACITY.
+ * PETALS_ERR_UNSUPPORTED; temperature at least 1e-38 and not infinite; M <= max_rows_per_call, else PETALS_ERR_CAPACITY.
  */
 int petals_client_distill(petals_client *client, const float *logits, int32_t M, const int32_t *teacher_tokens,
                           const float *teacher_logits, int32_t K, float temperature, const float *loss_grad,

@@ -17,7 +17,10 @@ namespace {
 // t = (l - m) / T, and rescales the two when m grows.  The exponentials are fp32 (base 2: x = t log2(e), D in that unit as
 // well); the sums are fp64, so that S - 1, what is left beside the largest token, keeps its digits where that token has
 // nearly everything: log S and -D / S are the two parts of the entropy, both >= 0, and nothing cancels between them.
-constexpr double LN2 = 0.69314718055994530942;
+//
+// Bound by the bytes of the logits where there are many rows: 1024 x 250880 with the 20 best of each in 210 us, 4.9 TB/s (a copy
+// within the memory reaches 4.8); with few rows by the latency of two launches, 1 x 250880 in 12 us.
+constexpr double LN2 = 0.69314718055994530942, LOG2E = 1.4426950408889634074;
 
 struct RowStat {
     float m;
@@ -28,7 +31,7 @@ struct RowStat {
 __device__ __forceinline__ void rescale(RowStat &s, float m, double invT) {
     if (s.m != -INFINITY) {
         const double t = ((double)s.m - m) * invT, e = exp_f64(t);
-        s.D = e * fma(t / LN2, s.S, s.D);
+        s.D = e * fma(t * LOG2E, s.S, s.D);
         s.S *= e;
     }
     s.m = m;
@@ -74,6 +77,9 @@ __device__ __forceinline__ float accumulate(RowStat &s, const float (&l)[N], flo
 constexpr int ROW_NT = 256, ROW_NW = ROW_NT / 64;
 constexpr int ROW_PER = 16;                         // logits of a thread per step
 constexpr int WAVE_STEP = 64 * ROW_PER, ROW_STEP = ROW_NW * WAVE_STEP;
+// Workgroups that a call is cut into at least, if it has the steps: 4 and 8 per compute unit.  (Log probabilities of 1024 x 250880
+// with 1024, 2048: 218, 255 us, each split starts a list of its own; distillation of 2048 x 250880 with 1024, 2048, 4096, 8192: 934,
+// 895, 913, 930.)
 constexpr int LOGPROBS_GROUPS = 1024, DISTILL_GROUPS = 2048;
 typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));     // rows of an odd vocabulary begin anywhere
 
@@ -198,7 +204,7 @@ __global__ void __launch_bounds__(ROW_NT) k_logprobs(LogprobsOut o, int V, int r
     __shared__ RowStat sm[ROW_NW];
     __shared__ uint64_t lists[ROW_NW][64];
     const int t = blockIdx.y, lane = threadIdx.x & 63, begin = blockIdx.x * range, end = min(V, begin + range);
-    const float c = (float)(invT / LN2);
+    const float c = (float)(invT * LOG2E);
     RowStat s{-INFINITY, 0.0, 0.0};
     TopList list;
     walk_row(o.logits + (size_t)t * V, begin, end, [&](int v0, const float (&l)[ROW_PER]) {
@@ -244,8 +250,12 @@ __global__ void __launch_bounds__(JOIN_NT) k_logprobs_join(LogprobsOut o, int V,
 // ------------------------------------------------------------------------------------ distillation
 //
 // Two passes over the logits: the softmax statistics, then w q.  A call goes through its rows in groups whose logits fit the
-// cache in front of the memory, so that the second pass need not ask the memory again: launch k takes the first pass of
-// group k and the second of group k - 1, whose reads and writes then share the launch.
+// 256 MB of cache in front of the memory, so that the second pass need not ask the memory again: launch k takes the first pass of
+// group k and the second of group k - 1, whose workgroups take turns, so that reads and writes share the launch.  The second pass
+// is the last to look at the logits and says so with its loads.  2048 x 250880: 895 us, what a copy of the logits takes is 860; in
+// one group 1119 us; the two kinds one after the other 1027; second pass with ordinary loads 1181; groups of 64, 96, 128, 144, 192
+// MB (before the number of workgroups was settled) 1052, 1013, 949, 979, 982.  Calls that fit as a whole are two launches (701 x
+// 50257, 141 MB: 80 us, in two groups 97).
 struct DistillIn {
     const float *logits;
     const int32_t *ids;
@@ -264,6 +274,8 @@ struct DistillRow {                    // of a row, by the workgroup of its firs
     double term, mass;                 // sum p (log p - z / T) and sum p: with log q = z / T - lse the loss is T^2 (term + mass lse)
     int listed;
 };
+constexpr int MAX_GRID_ROWS = 1 << 14;      // rows of a group (two groups share the grid's second dimension)
+constexpr size_t DISTILL_GROUP = (size_t)128 << 20, DISTILL_ONE_GROUP = (size_t)192 << 20;
 constexpr int LIST_PER = (PETALS_DISTILL_TOP_MAX + ROW_NT - 1) / ROW_NT;
 
 // entry k of a row's list; an entry that counts for nothing has value -infinity
@@ -278,7 +290,7 @@ __device__ __forceinline__ float teacher_entry(const DistillIn &d, int t, int k,
 __device__ __forceinline__ void distill_stats(const DistillIn &d, int t, DistillPart *__restrict__ part, DistillRow *__restrict__ out,
                                               RowStat *sm, double *sd, float *sf) {
     const float *row = d.logits + (size_t)t * d.V;
-    const float c = (float)(d.invT / LN2);
+    const float c = (float)(d.invT * LOG2E);
     const int begin = blockIdx.x * d.range, end = min(d.V, begin + d.range);
     float val[LIST_PER], mx = -INFINITY;
     int id[LIST_PER];
@@ -331,7 +343,7 @@ __device__ __forceinline__ void distill_grad(const DistillIn &d, int t, const Di
                                              int *s_id, double *s_p) {
     const int lane = threadIdx.x & 63, splits = gridDim.x;
     const float *row = d.logits + (size_t)t * d.V;
-    const float c = (float)(d.invT / LN2);
+    const float c = (float)(d.invT * LOG2E);
     const int begin = blockIdx.x * d.range, end = min(d.V, begin + d.range);
     if (!d.grad && blockIdx.x) return;
     const DistillRow r = rows[t];
@@ -418,7 +430,7 @@ __global__ void __launch_bounds__(ROW_NT) k_distill(DistillIn d, int first2, int
     __shared__ float sf[ROW_NW];
     __shared__ int s_id[PETALS_DISTILL_TOP_MAX];
     __shared__ double s_p[PETALS_DISTILL_TOP_MAX];
-    // the two kinds take turns, as far as there are both
+    // as far as there are both kinds they take turns
     const int y = blockIdx.y, n1 = (int)gridDim.y - n2, both = 2 * min(n1, n2);
     const bool second = y < both ? !(y & 1) : both ? n2 > n1 : y < n2;
     const int i = y < both ? y >> 1 : both ? y - both / 2 : second ? y : y - n2;
@@ -604,11 +616,10 @@ void embed_backward(const __half *grad, int M, int H, const __half *E, const __h
 int check_call(const petals_client_config &cfg, int32_t M) {
     if (M < 1) return ps_fail(PETALS_ERR_INVALID_ARG, "M must be positive");
     if (M > cfg.max_rows_per_call) return ps_fail(PETALS_ERR_CAPACITY, "%d rows exceed max_rows_per_call %d", M, cfg.max_rows_per_call);
+    if (cfg.vocab > 1 << 30) return ps_fail(PETALS_ERR_UNSUPPORTED, "vocabulary %d exceeds 2^30", cfg.vocab);
     return PETALS_OK;
 }
-constexpr int MAX_GRID_ROWS = 1 << 14;      // rows of a group (two groups share the grid's second dimension)
-constexpr size_t DISTILL_GROUP = (size_t)128 << 20, DISTILL_ONE_GROUP = (size_t)192 << 20;
-bool usable_temperature(float t) { return t > 0.0f && t < INFINITY && 1.0f / t < INFINITY; }
+bool usable_temperature(float t) { return t >= 1e-38f && t < INFINITY; }     // (log2(e) / t is a number in fp32)
 
 }  // namespace
 

@@ -305,15 +305,18 @@ HeadPlan head_plan(const petals_client_config &cfg, int M) {
     return p;
 }
 
-// The limit of a kernel's dynamic LDS belongs to the function, for the whole process: set once
+// The limit of a kernel's dynamic LDS belongs to the function on a GPU, for the whole process: set once for each
 struct LdsLimit {
+    static constexpr int MOST = 64;
     std::mutex lock;
-    bool set = false;
+    bool set[MOST] = {};
     hipError_t allow(const void *kernel, int bytes) {
+        int gpu = 0;
+        if (hipError_t e = hipGetDevice(&gpu)) return e;
         std::lock_guard<std::mutex> hold(lock);
-        if (set) return hipSuccess;
+        if (gpu < MOST && set[gpu]) return hipSuccess;
         const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-        set = e == hipSuccess;
+        if (gpu < MOST) set[gpu] = e == hipSuccess;
         return e;
     }
 };
@@ -338,6 +341,14 @@ hipError_t head_block(const HeadPlan &p, const __half *E, uint8_t *store, int M,
     return hipGetLastError();
 }
 
+int check_rows(const petals_client_config &cfg, int32_t M) {
+    if (M < 1) return ps_fail(PETALS_ERR_INVALID_ARG, "M must be positive");
+    if (M > cfg.max_rows_per_call) return ps_fail(PETALS_ERR_CAPACITY, "%d rows exceed max_rows_per_call %d", M, cfg.max_rows_per_call);
+    if (M > PETALS_BACKWARD_ROWS_MAX) return ps_fail(PETALS_ERR_UNSUPPORTED, "%d rows exceed %d", M, PETALS_BACKWARD_ROWS_MAX);
+    if (cfg.vocab > 1 << 30) return ps_fail(PETALS_ERR_UNSUPPORTED, "vocabulary %d exceeds 2^30", cfg.vocab);
+    return PETALS_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -345,9 +356,7 @@ extern "C" {
 int petals_client_lm_head_backward_bytes(const petals_client_config *cfg, int32_t M, size_t *bytes) {
     if (!bytes) return ps_fail(PETALS_ERR_INVALID_ARG, "null pointer");
     if (int rc = ps_check_client_config(cfg)) return rc;
-    if (M < 1) return ps_fail(PETALS_ERR_INVALID_ARG, "M must be positive");
-    if (M > cfg->max_rows_per_call) return ps_fail(PETALS_ERR_CAPACITY, "%d rows exceed max_rows_per_call %d", M, cfg->max_rows_per_call);
-    if (M > PETALS_BACKWARD_ROWS_MAX) return ps_fail(PETALS_ERR_UNSUPPORTED, "%d rows exceed %d", M, PETALS_BACKWARD_ROWS_MAX);
+    if (int rc = check_rows(*cfg, M)) return rc;
     *bytes = head_plan(*cfg, M).bytes;
     return PETALS_OK;
 }
@@ -357,9 +366,7 @@ int petals_client_lm_head_backward(petals_client *client, void *dev_store, const
     if (!client || !dev_store || !hidden_in || !grad_logits || !grad_hidden_out) return ps_fail(PETALS_ERR_INVALID_ARG, "null pointer");
     if ((uintptr_t)dev_store & 255) return ps_fail(PETALS_ERR_INVALID_ARG, "store must be 256-byte aligned");
     const ps_client_view c = ps_view(client);
-    if (M < 1) return ps_fail(PETALS_ERR_INVALID_ARG, "M must be positive");
-    if (M > c.cfg->max_rows_per_call) return ps_fail(PETALS_ERR_CAPACITY, "%d rows exceed max_rows_per_call %d", M, c.cfg->max_rows_per_call);
-    if (M > PETALS_BACKWARD_ROWS_MAX) return ps_fail(PETALS_ERR_UNSUPPORTED, "%d rows exceed %d", M, PETALS_BACKWARD_ROWS_MAX);
+    if (int rc = check_rows(*c.cfg, M)) return rc;
     if (grad_hidden_out == hidden_in || grad_hidden_out == (const void *)grad_logits)
         return ps_fail(PETALS_ERR_INVALID_ARG, "buffers alias");
     const HeadPlan p = head_plan(*c.cfg, M);
