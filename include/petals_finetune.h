@@ -77,8 +77,9 @@ int petals_client_distill(petals_client *client, const float *logits, int32_t M,
  *   grad_hidden_out   dev fp16 [M, H]: grad_out of petals_span_backward; may not overlap the inputs
  * (The roundings of the forward pass count as the identity; matrix and LayerNorm parameters are frozen.)  The product runs on
  * fp16 matrix instructions with fp32 sums; grad_logits is taken as two fp16 values for calls of up to
- * PETALS_HEAD_BACKWARD_PAIR_ROWS rows and as one beyond, scaled per row and section of the vocabulary so that the section's
- * largest value is exact and values down to 2^-28 of it are rounded at 2^-12 of themselves.  grad_hidden_out is rounded to
+ * PETALS_HEAD_BACKWARD_PAIR_ROWS rows and as one beyond, scaled per row and section of the vocabulary (1024 columns, beyond
+ * those rows 2048) so that the section's largest value is exact and one value rounds by at most 2^-11 of itself down to 2^-29 of
+ * the largest, two by 2^-22 down to 2^-18.  grad_hidden_out is rounded to
  * fp16 once, without loss scaling (loss_grad of petals_client_distill can carry a scale).
  * dev_store: 256-byte aligned device memory of petals_client_lm_head_backward_bytes(cfg, M) bytes, contents unspecified
  * before and after.  M <= max_rows_per_call, else PETALS_ERR_CAPACITY.
@@ -97,7 +98,7 @@ int petals_client_lm_head_backward(petals_client *client, void *dev_store, const
  *   grads_out         dev fp32 [M, H]: row i = the gradient of embeddings[tokens_out[i]], through the LayerNorm behind the lookup
  *   count_out         dev int32 [1]: how many there are; entries of the two outputs from there on are left as they were
  * The rows of a token are summed in fp32 in the order of their positions (long lists in pieces), then go through the
- * derivative of the LayerNorm once.  M <= max_rows_per_call, else PETALS_ERR_CAPACITY.
+ * derivative of the LayerNorm once.  Outputs may not overlap the inputs.  M <= max_rows_per_call, else PETALS_ERR_CAPACITY.
  */
 int petals_client_embed_backward(petals_client *client, const int32_t *token_ids, const void *grad_hidden, int32_t M,
                                  int32_t *tokens_out, float *grads_out, int32_t *count_out, void *stream);

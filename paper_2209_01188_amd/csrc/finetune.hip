@@ -18,7 +18,7 @@ namespace {
 // well); the sums are fp64, so that S - 1, what is left beside the largest token, keeps its digits where that token has
 // nearly everything: log S and -D / S are the two parts of the entropy, both >= 0, and nothing cancels between them.
 //
-// Bound by the bytes of the logits where there are many rows: 1024 x 250880 with the 20 best of each in 210 us, 4.9 TB/s (a copy
+// Bound by the bytes of the logits where there are many rows: 1024 x 250880 with the 20 best of each in 199 us, 5.2 TB/s (a copy
 // within the memory reaches 4.8); with few rows by the latency of two launches, 1 x 250880 in 12 us.
 constexpr double LN2 = 0.69314718055994530942, LOG2E = 1.4426950408889634074;
 
@@ -65,12 +65,14 @@ __device__ __forceinline__ float accumulate(RowStat &s, const float (&l)[N], flo
     for (int i = 1; i < N; i++) cm = fmaxf(cm, l[i]);
     if (cm > s.m) rescale(s, cm, invT);
     const float m = s.m == -INFINITY ? 0.0f : s.m;
+    float d = 0.0f;                                                          // (a step's terms have one sign: their sum in fp32 is off by 2^-20 of itself)
 #pragma unroll
     for (int i = 0; i < N; i++) {
         const float x = (l[i] - m) * c, e = __builtin_amdgcn_exp2f(x);
         s.S += (double)e;
-        if (WITH_D) s.D += (double)(e * fmaxf(x, -1e30f));                    // (a token ruled out: 0 times a number)
+        if (WITH_D) d = fmaf(e, fmaxf(x, -1e30f), d);                         // (a token ruled out: 0 times a number)
     }
+    if (WITH_D) s.D += (double)d;
     return cm;
 }
 
@@ -458,48 +460,43 @@ constexpr int PLACE_ROWS = 16;        // positions of a workgroup, compared with
 // first: a byte per place, 1 where a token begins
 __global__ void __launch_bounds__(1024) k_token_places(const int32_t *__restrict__ ids, int M, int V, Place *__restrict__ places,
                                                        uint8_t *__restrict__ first) {
-    __shared__ __align__(16) int tile[1024];
+    constexpr int TILE = 4096;                         // ids in LDS at a time
+    __shared__ __align__(16) int tile[TILE];
     __shared__ int sums[3][64][PLACE_ROWS];
     const int g = threadIdx.x / PLACE_ROWS, r = threadIdx.x % PLACE_ROWS, i0 = blockIdx.x * PLACE_ROWS, i = i0 + r;
     const int own = min(max(ids[min(i, M - 1)], 0), V - 1);
-    int n_less = 0, n_before = 0, n_all = 0;
-    for (int j0 = 0; j0 < M; j0 += 1024) {
-        const int j = j0 + threadIdx.x;
+    int place = 0, n_before = 0, n_all = 0;
+    for (int j0 = 0; j0 < M; j0 += TILE) {
+        const int here = min(TILE, (M - j0 + 3) / 4 * 4);
         __syncthreads();
-        tile[threadIdx.x] = j < M ? min(max(ids[j], 0), V - 1) : 0x7fffffff;       // (no token)
+        for (int u = threadIdx.x; u < here; u += 1024) tile[u] = j0 + u < M ? min(max(ids[j0 + u], 0), V - 1) : 0x7fffffff;      // (no token)
         __syncthreads();
-        const v4i *mine = (const v4i *)tile + g * 4;
-        if (j0 + 1024 <= i0 || j0 >= i0 + PLACE_ROWS) {                            // all of them before, or behind, these positions
-            const int border = own + (j0 < i0);
-            int n = 0;
-#pragma unroll
-            for (int q = 0; q < 4; q++) {
-                const v4i o = mine[q];
+        // four ids at a time; of those before this workgroup's positions equal ones count as less, of its own those before i
+        for (int q = g * 4; q < here; q += 256) {
+            const v4i o = *(const v4i *)(tile + q);
+            const int j = j0 + q;
+            if (j + 4 <= i0 || j >= i0 + PLACE_ROWS) {
+                const int border = own + (j < i0);
+                int n = 0;
 #pragma unroll
                 for (int e = 0; e < 4; e++) {
-                    n_less += o[e] < border;
+                    place += o[e] < border;
                     n += o[e] == own;
                 }
-            }
-            n_all += n;
-            if (j0 < i0) {                                                          // (n_less has them already)
-                n_before += n;
-                n_less -= n;
-            }
-        } else {
-#pragma unroll
-            for (int q = 0; q < 4; q++) {
-                const v4i o = mine[q];
+                n_all += n;
+                n_before += j < i0 ? n : 0;
+            } else {
 #pragma unroll
                 for (int e = 0; e < 4; e++) {
-                    n_less += o[e] < own;
-                    n_all += o[e] == own;
-                    n_before += o[e] == own && j0 + g * 16 + q * 4 + e < i;
+                    const bool same = o[e] == own, before = same && j + e < i;
+                    place += o[e] < own || before;
+                    n_all += same;
+                    n_before += before;
                 }
             }
         }
     }
-    sums[0][g][r] = n_less;
+    sums[0][g][r] = place;
     sums[1][g][r] = n_before;
     sums[2][g][r] = n_all;
     __syncthreads();
@@ -514,8 +511,8 @@ __global__ void __launch_bounds__(1024) k_token_places(const int32_t *__restrict
             n[c] = group_reduce<4>(n[c], [](uint32_t a, uint32_t b) { return a + b; });
         }
         if (part == 0 && i0 + p < M) {
-            places[n[0] + n[1]] = Place{i0 + p, token, (int)n[1], (int)n[2]};
-            first[n[0] + n[1]] = n[1] == 0;
+            places[n[0]] = Place{i0 + p, token, (int)n[1], (int)n[2]};
+            first[n[0]] = n[1] == 0;
         }
     }
 }
@@ -523,14 +520,17 @@ __global__ void __launch_bounds__(1024) k_token_places(const int32_t *__restrict
 // How many pieces a list of n positions has, each of RUN_PIECE but the last, which takes what is left over as well
 __device__ __forceinline__ int run_pieces(int n) { return max(1, n / RUN_PIECE); }
 
-// number of different tokens before place p, over the workgroup, in two parts with a barrier between them; first is padded to 8 bytes
+// Number of different tokens before place p, over the workgroup: each thread's first flags (8 places; first is padded to that) asked
+// for early, then the waves' sums, and behind a barrier all of them.
+__device__ __forceinline__ uint64_t token_flags(const uint8_t *__restrict__ first, int p, int q) {
+    if (q >= p) return 0;
+    const uint64_t w = *(const uint64_t *)(first + q);
+    return p - q >= 8 ? w : w & ((1ull << (8 * (p - q))) - 1);
+}
 template <int NT>
-__device__ __forceinline__ void count_tokens(const uint8_t *__restrict__ first, int p, int *sm) {
-    int n = 0;
-    for (int q = threadIdx.x * 8; q < p; q += NT * 8) {
-        const uint64_t w = *(const uint64_t *)(first + q);
-        n += __popcll(p - q >= 8 ? w : w & ((1ull << (8 * (p - q))) - 1));
-    }
+__device__ __forceinline__ void count_tokens(const uint8_t *__restrict__ first, int p, uint64_t flags, int *sm) {
+    int n = __popcll(flags);
+    for (int q = (threadIdx.x + NT) * 8; q < p; q += NT * 8) n += __popcll(token_flags(first, p, q));
     const float of_wave = wave_sum((float)n);                        // at most 2^24 of them
     if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = (int)of_wave;
 }
@@ -546,13 +546,13 @@ __global__ void __launch_bounds__(NT) k_embed_backward(const __half *__restrict_
                                                        const Place *__restrict__ places, const uint8_t *__restrict__ first,
                                                        float *__restrict__ parts, int32_t *__restrict__ tokens_out,
                                                        float *__restrict__ grads_out, int32_t *__restrict__ count_out) {
-    __shared__ double sd[NT / 64][2];
+    __shared__ double sd[NT / 64][4];
     __shared__ int si[NT / 64];
     const int p = blockIdx.x;
     const Place pl = places[p];
     const int piece = pl.before / RUN_PIECE, pieces = run_pieces(pl.count);
     if (p == M - 1) {
-        count_tokens<NT>(first, M, si);
+        count_tokens<NT>(first, M, token_flags(first, M, threadIdx.x * 8), si);
         __syncthreads();
         const int n = counted_tokens<NT>(si);
         if (threadIdx.x == 0) *count_out = n;
@@ -561,14 +561,19 @@ __global__ void __launch_bounds__(NT) k_embed_backward(const __half *__restrict_
     if (pl.before % RUN_PIECE || piece >= pieces) return;
     const int n = piece == pieces - 1 ? pl.count - pl.before : RUN_PIECE;
     LnRow<PER> row;
-    if (pieces == 1) ln_load<NT, PER>(row, E + (size_t)pl.token * H, g, H);
+    uint64_t flags = 0;
+    if (pieces == 1) {
+        flags = token_flags(first, p, threadIdx.x * 8);
+        ln_load<NT, PER>(row, E + (size_t)pl.token * H, g, H);
+    }
     float acc[PER][8] = {};
-    add_rows<NT, PER, _Float16>(acc, n, H, [&](int r) { return (const _Float16 *)grad + (size_t)places[p + r].position * H; });
+    add_some_rows<NT, PER, _Float16, 1>(acc, 0, H, [&](int) { return (const _Float16 *)grad + (size_t)pl.position * H; });
+    add_rows<NT, PER, _Float16, 8>(acc, n - 1, H, [&](int r) { return (const _Float16 *)grad + (size_t)places[p + 1 + r].position * H; });
     if (pieces > 1) {                                                // pieces begin at least RUN_PIECE places apart
         ln_store<NT, PER>(acc, parts + (size_t)(p / RUN_PIECE) * H, H);
         return;
     }
-    count_tokens<NT>(first, p, si);
+    count_tokens<NT>(first, p, flags, si);
     ln_backward<NT, PER>(acc, row, H, eps, sd);
     const int u = counted_tokens<NT>(si);
     ln_store<NT, PER>(acc, grads_out + (size_t)u * H, H);
@@ -581,7 +586,7 @@ __global__ void __launch_bounds__(NT) k_embed_backward_join(int M, int H, const 
                                                             const Place *__restrict__ places, const uint8_t *__restrict__ first,
                                                             const float *__restrict__ parts, int32_t *__restrict__ tokens_out,
                                                             float *__restrict__ grads_out) {
-    __shared__ double sd[NT / 64][2];
+    __shared__ double sd[NT / 64][4];
     __shared__ int si[NT / 64];
     const int lane = threadIdx.x & 63, q = blockIdx.x * RUN_PIECE + lane;
     bool begins = false;
@@ -594,10 +599,11 @@ __global__ void __launch_bounds__(NT) k_embed_backward_join(int M, int H, const 
     const int p = blockIdx.x * RUN_PIECE + __builtin_ctzll(who);
     const Place pl = places[p];
     LnRow<PER> row;
+    const uint64_t flags = token_flags(first, p, threadIdx.x * 8);
     ln_load<NT, PER>(row, E + (size_t)pl.token * H, g, H);
     float acc[PER][8] = {};
-    add_rows<NT, PER, float>(acc, run_pieces(pl.count), H, [&](int r) { return parts + (size_t)(p / RUN_PIECE + r) * H; });
-    count_tokens<NT>(first, p, si);
+    add_rows<NT, PER, float, 4>(acc, run_pieces(pl.count), H, [&](int r) { return parts + (size_t)(p / RUN_PIECE + r) * H; });
+    count_tokens<NT>(first, p, flags, si);
     ln_backward<NT, PER>(acc, row, H, eps, sd);
     const int u = counted_tokens<NT>(si);
     ln_store<NT, PER>(acc, grads_out + (size_t)u * H, H);

@@ -15,8 +15,8 @@ namespace {
 typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));     // rows of an odd vocabulary begin anywhere
 
 // G as fp16 in the operand order of v_mfma_f32_16x16x32_f16: tile (mt, kt) of 16 rows x 32 columns is 1 KB, lane slot
-// 16 (column / 8) + row holds 8 columns.  A row's section is scaled so that its largest value becomes 32768: fp16 then keeps
-// 2^-12 of a value down to 2^-29 of the largest (a softmax's gradient reaches from 1 down to 1e-9 and less), and the largest,
+// 16 (column / 8) + row holds 8 columns.  A row's section is scaled so that its largest value becomes 32768: fp16 then rounds
+// by at most 2^-11 of a value down to 2^-29 of the largest (a softmax's gradient reaches from 1 down to 1e-9 and less), and the largest,
 // mostly the label's, exactly.  lo (may be null): what the rounding left, in the same scale.
 // A wave per row and section, SKT k-tiles: it reads 1 KB of the row at a time (a row of an odd vocabulary begins anywhere; the
 // tiles' own 128 bytes of it would touch two lines each), takes the maximum, and drops its halves into LDS where the tiles lie;
@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(512, 2) k_head_block(const __half *__restrict_
 template <int NT, int PER>
 __global__ void __launch_bounds__(NT) k_head_finish(const float *__restrict__ part, int splits, int M, int H, const __half *__restrict__ x,
                                                     const __half *__restrict__ g, float eps, __half *__restrict__ out) {
-    __shared__ double sm[NT / 64][2];
+    __shared__ double sm[NT / 64][4];
     const int t = blockIdx.x;
     LnRow<PER> lr;
     ln_load<NT, PER>(lr, x + (size_t)t * H, g, H);
