@@ -25,11 +25,12 @@ typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));     // ro
 constexpr int PACK_GROUP = 16 * 16 + 16, PACK_TILE = 4 * PACK_GROUP;
 constexpr int head_section_kt(bool pair) { return pair ? 32 : 64; }
 template <bool PAIR>
-__global__ void __launch_bounds__(1024) k_head_pack(const float *__restrict__ G, int M, int V, int KT,
+__global__ void __launch_bounds__(1024) k_head_pack(const float *__restrict__ G, int M, int V, int KT, int sections,
                                                     __half *__restrict__ hi, __half *__restrict__ lo, float *__restrict__ unit) {
     extern __shared__ __align__(16) unsigned char lds[];
     constexpr int SKT = head_section_kt(PAIR), STEPS = SKT / 8;
-    const int sec = blockIdx.x, mt = blockIdx.y, lane = threadIdx.x & 63, r = threadIdx.x >> 6, t = mt * 16 + r, v0 = sec * SKT * 32 + lane * 4;
+    const int mt = __builtin_amdgcn_readfirstlane(blockIdx.x / sections), sec = blockIdx.x - mt * sections, MTT = (M + 15) >> 4;
+    const int lane = threadIdx.x & 63, r = threadIdx.x >> 6, t = mt * 16 + r, v0 = sec * SKT * 32 + lane * 4;
     const float *row = G + (size_t)min(t, M - 1) * V;
     float f[STEPS][4];
     float mx = 0.0f;
@@ -52,7 +53,7 @@ __global__ void __launch_bounds__(1024) k_head_pack(const float *__restrict__ G,
     mx = wave_max(mx);
     // (rows behind the call's, sections of zeros and of next to nothing: a unit of 2^-60, so that the ratio of two units stays a number)
     const float u = t < M ? fmaxf(mx * 0x1p-15f, 0x1p-60f) : 0x1p-60f, s = t < M ? 1.0f / u : 0.0f;
-    if (lane == 0) unit[(size_t)sec * gridDim.y * 16 + t] = u;
+    if (lane == 0) unit[(size_t)sec * MTT * 16 + t] = u;
     unsigned char *mine = lds + (lane >> 3) * PACK_TILE + ((lane & 7) >> 1) * PACK_GROUP + r * 16 + (lane & 1) * 8;
 #pragma unroll
     for (int i = 0; i < STEPS; i++) {
@@ -326,8 +327,8 @@ hipError_t head_pack(const HeadPlan &p, const float *G, uint8_t *store, int M, i
     constexpr int bytes = head_section_kt(PAIR) * PACK_TILE * (PAIR ? 2 : 1);
     static LdsLimit limit;
     if (hipError_t e = limit.allow((const void *)k_head_pack<PAIR>, bytes)) return e;
-    k_head_pack<PAIR><<<dim3(p.sections, p.mtt), 1024, bytes, st>>>(G, M, V, p.kt, (__half *)(store + p.hi), (__half *)(store + p.lo),
-                                                                        (float *)(store + p.unit));
+    k_head_pack<PAIR><<<p.sections * p.mtt, 1024, bytes, st>>>(G, M, V, p.kt, p.sections, (__half *)(store + p.hi), (__half *)(store + p.lo),
+                                                               (float *)(store + p.unit));
     return hipGetLastError();
 }
 template <int BM, bool PAIR>

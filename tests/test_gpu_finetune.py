@@ -432,3 +432,70 @@ def test_calls_on_another_stream():
     assert np.allclose(to_np(lp), of.logprobs(x, tokens)[0], rtol=1e-5, atol=1e-5)
     assert np.allclose(to_np(loss), -to_np(lp), rtol=1e-6, atol=1e-6)
     c.close()
+
+
+def test_offsets_beyond_32_bits():
+    """More than 2^32 logits: the rows at the end come out as the same rows do in a call of their own."""
+    V, H, M, K = 250880, 64, 17200, 3                      # 4.3e9 logits, 17 GB; and more rows than one launch takes
+    c, E, vec = _client(V, H, M, seed=21)
+    r = np.random.default_rng(22)
+    base = to_dev((r.standard_normal((1 << 20) + 7)).astype(np.float32) * 3)
+    x = torch.empty((M, V), device=DEV)
+    flat, n = x.view(-1), base.numel()                     # (a period prime to V: no two rows alike)
+    whole = flat.numel() // n * n
+    flat[:whole].view(-1, n).copy_(base)
+    flat[whole:] = base[:flat.numel() - whole]
+    rows = [0, 1, 16383, 16384, 17119, 17198, 17199]       # 2^32 logits end in row 17119
+    own = x[rows].contiguous()
+    tokens = r.integers(0, V, M).astype(np.int32)
+    lp, ent, top, tlp = c.logprobs(x, to_dev(tokens), 1.0, 5)
+    rlp, rent, rtop, rtlp = of.logprobs(to_np(own), tokens[rows], 1.0, 5)
+    rel = _rel(to_np(own), 1.0)
+    assert np.array_equal(to_np(top)[rows], rtop)
+    assert (np.abs(to_np(lp)[rows] - rlp) <= U32 * np.abs(rlp) + rel).all()
+    assert (np.abs(to_np(ent)[rows] - rent) <= 2 * (rel + 2 * U32) * rent).all()
+
+    ids = r.integers(0, V, (M, K)).astype(np.int32)
+    vals = r.standard_normal((M, K)).astype(np.float32)
+    loss, grad = c.distill(x, to_dev(ids), to_dev(vals), grad_out=x)          # in place
+    want_loss, want = c.distill(own, to_dev(ids[rows]), to_dev(vals[rows]))
+    mine = grad[rows].contiguous()
+    # (a row is cut into other parts in a call of few rows: the same sums in fp64, of exponentials about other maxima)
+    assert (np.abs(to_np(loss)[rows] - to_np(want_loss)) <= (2 * rel + 2 * U32) * np.abs(to_np(want_loss)) + 2 * rel).all()
+    assert (np.abs(to_np(mine) - to_np(want)) <= 2 * (rel[:, None] + U32) * np.abs(to_np(want)) + 2.0 ** -126).all()
+
+    hid = r.standard_normal((M, H)).astype(np.float16)
+    out = to_np(c.lm_head_backward(to_dev(hid), grad))
+    G = to_np(mine)
+    ref = of.lm_head_backward(hid[rows], G, E, vec[2])
+    mass = np.abs(G).astype(np.float64) @ np.abs(E).astype(np.float64)
+    err = (U16 + (V / 32 + 40) * U32) * mass + np.abs(G).max(1, keepdims=True) * 2.0 ** -40 * np.abs(E).astype(np.float64).sum(0)
+    tol = _norm_error(err, hid[rows], vec[2]) + 2 * U16 * np.abs(ref) + 2.0 ** -25 + 1e-6 * np.abs(ref).max(1, keepdims=True)
+    assert (np.abs(out[rows].astype(np.float64) - ref) <= tol).all()
+    c.close()
+
+
+def test_the_most_rows_of_the_backward_calls():
+    """2^20 rows: 65536 token tiles of the head, tokens with long and short lists."""
+    V, H, M = 40, 64, 1 << 20
+    c, E, vec = _client(V, H, M, seed=23)
+    r = np.random.default_rng(24)
+    G = r.standard_normal((M, V)).astype(np.float32)
+    hid = r.standard_normal((M, H)).astype(np.float16)
+    out = to_np(c.lm_head_backward(to_dev(hid), to_dev(G))).astype(np.float64)
+    ref = of.lm_head_backward(hid, G, E, vec[2])
+    mass = np.abs(G).astype(np.float64) @ np.abs(E).astype(np.float64)
+    tol = _norm_error((U16 + 42 * U32) * mass + 2.0 ** -36, hid, vec[2]) + 2 * U16 * np.abs(ref) + 2.0 ** -25
+    assert (np.abs(out - ref) <= tol).all()
+
+    ids = np.minimum((r.random(M) ** 4 * V).astype(np.int32), V - 3)          # the last token: once; the one before: never
+    ids[12345] = V - 1
+    dy = r.integers(-8, 9, (M, H)).astype(np.float16)                         # sums below 2^24 are exact in fp32
+    tokens, grads, count = [to_np(a) for a in c.embed_backward(to_dev(ids), to_dev(dy))]
+    rtok, ref = of.embed_backward(ids, dy, E, vec[0])
+    n = len(rtok)
+    assert count[0] == n and np.array_equal(tokens[:n], rtok)
+    mass = np.abs(np.stack([np.bincount(ids, dy[:, j].astype(np.float64), V) for j in range(H)], 1))[rtok]
+    tol = _norm_error(2 * U32 * mass, E[rtok], vec[0]) + U32 * np.abs(ref) + 1e-12 * np.abs(ref).max()
+    assert (np.abs(grads[:n] - ref) <= tol).all()
+    c.close()
