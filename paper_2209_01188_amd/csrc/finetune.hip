@@ -454,7 +454,9 @@ __global__ void __launch_bounds__(ROW_NT) k_distill(DistillIn d, int first2, int
 struct __align__(16) Place {
     int position, token, before, count;      // a position and its token; how many earlier ones have the same, and how many in all
 };
-constexpr int RUN_PIECE = 32;         // positions that one workgroup sums; a longer list goes in pieces of 32 to 63
+// A token's list of fewer than RUN_PIECE positions is one workgroup's, the whole row of each.  A longer one goes in pieces of 32 to 63
+// positions, and a workgroup has 1024 columns of one: few tokens that stand everywhere are spread over the chip as well as many.
+constexpr int RUN_PIECE = 32, PIECE_COLUMNS = 1024;
 constexpr int PLACE_ROWS = 16;        // positions of a workgroup, compared with all of the call's by 64 groups of 16 threads
 
 // first: a byte per place, 1 where a token begins
@@ -517,8 +519,16 @@ __global__ void __launch_bounds__(1024) k_token_places(const int32_t *__restrict
     }
 }
 
-// How many pieces a list of n positions has, each of RUN_PIECE but the last, which takes what is left over as well
-__device__ __forceinline__ int run_pieces(int n) { return max(1, n / RUN_PIECE); }
+// How many pieces a list of n positions has, each of RUN_PIECE but the last, which takes what is left over as well (0: not in pieces).
+// Pieces begin at least RUN_PIECE places apart: their sums are row (place / RUN_PIECE) of `parts`.
+__device__ __forceinline__ int run_pieces(int n) { return n / RUN_PIECE; }
+// the one of places s RUN_PIECE .. + RUN_PIECE for which holds(place), -1: none; by every wave
+template <typename F>
+__device__ __forceinline__ int find_place(const Place *__restrict__ places, int s, int M, F holds) {
+    const int lane = threadIdx.x & 63, q = s * RUN_PIECE + lane;
+    const unsigned long long who = __ballot(lane < RUN_PIECE && q < M && holds(places[min(q, M - 1)]));
+    return who ? s * RUN_PIECE + __builtin_ctzll(who) : -1;
+}
 
 // Number of different tokens before place p, over the workgroup: each thread's first flags (8 places; first is padded to that) asked
 // for early, then the waves' sums, and behind a barrier all of them.
@@ -540,47 +550,69 @@ __device__ __forceinline__ int counted_tokens(const int *sm) {
     return (int)wave_sum(lane < NT / 64 ? (float)sm[lane] : 0.0f);
 }
 
-// one workgroup per place: a place at which a piece of a token's list begins has work
+// One workgroup for each RUN_PIECE places and PIECE_COLUMNS columns, in which a piece may begin; behind those (`pieces` of them) one per
+// place, at which a token with a short list may begin.
 template <int NT, int PER>
-__global__ void __launch_bounds__(NT) k_embed_backward(const __half *__restrict__ grad, int M, int H, const __half *__restrict__ E, const __half *__restrict__ g, float eps,
-                                                       const Place *__restrict__ places, const uint8_t *__restrict__ first,
+__global__ void __launch_bounds__(NT, PER == 1 ? 8 : 4) k_embed_backward(const __half *__restrict__ grad, int M, int H, const __half *__restrict__ E, const __half *__restrict__ g, float eps,
+                                                       const Place *__restrict__ places, const uint8_t *__restrict__ first, int pieces,
                                                        float *__restrict__ parts, int32_t *__restrict__ tokens_out,
                                                        float *__restrict__ grads_out, int32_t *__restrict__ count_out) {
-    __shared__ double sd[NT / 64][4];
-    __shared__ int si[NT / 64];
-    const int p = blockIdx.x;
-    const Place pl = places[p];
-    const int piece = pl.before / RUN_PIECE, pieces = run_pieces(pl.count);
-    if (p == M - 1) {
-        count_tokens<NT>(first, M, token_flags(first, M, threadIdx.x * 8), si);
+    constexpr int COLS = PIECE_COLUMNS / 8, GROUPS = NT / COLS;
+    __shared__ union __align__(16) {
+        struct {
+            double sd[NT / 64][4];
+            int si[NT / 64];
+        };
+        float sums[GROUPS][PIECE_COLUMNS];
+    } sm;
+    if ((int)blockIdx.x < pieces) {
+        const int per = (H + PIECE_COLUMNS - 1) / PIECE_COLUMNS, s = blockIdx.x / per, c0 = (blockIdx.x - s * per) * PIECE_COLUMNS;
+        const int p = find_place(places, s, M, [](const Place &pl) { return pl.before % RUN_PIECE == 0 && pl.before / RUN_PIECE < run_pieces(pl.count); });
+        if (p < 0) return;
+        const Place pl = places[p];
+        const int n = pl.before / RUN_PIECE == run_pieces(pl.count) - 1 ? pl.count - pl.before : RUN_PIECE;
+        const int group = threadIdx.x / COLS, k0 = c0 + threadIdx.x % COLS * 8;
+        float acc[1][8] = {};
+        add_rows<NT, 1, _Float16, 4>(acc, (n - group + GROUPS - 1) / GROUPS, k0, H,
+                                     [&](int r) { return (const _Float16 *)grad + (size_t)places[p + group + GROUPS * r].position * H; });
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+            *(v4f *)&sm.sums[group][threadIdx.x % COLS * 8 + 4 * h] = v4f{acc[0][4 * h], acc[0][4 * h + 1], acc[0][4 * h + 2], acc[0][4 * h + 3]};
         __syncthreads();
-        const int n = counted_tokens<NT>(si);
+        for (int k = threadIdx.x; k < min(PIECE_COLUMNS, H - c0); k += NT) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < GROUPS; i++) sum += sm.sums[i][k];
+            parts[(size_t)s * H + c0 + k] = sum;
+        }
+        return;
+    }
+    const int p = blockIdx.x - pieces;
+    const Place pl = places[p];
+    if (p == M - 1) {
+        count_tokens<NT>(first, M, token_flags(first, M, threadIdx.x * 8), sm.si);
+        __syncthreads();
+        const int n = counted_tokens<NT>(sm.si);
         if (threadIdx.x == 0) *count_out = n;
         __syncthreads();
     }
-    if (pl.before % RUN_PIECE || piece >= pieces) return;
-    const int n = piece == pieces - 1 ? pl.count - pl.before : RUN_PIECE;
+    if (pl.before || run_pieces(pl.count)) return;
+    const uint64_t flags = token_flags(first, p, threadIdx.x * 8);
     LnRow<PER> row;
-    uint64_t flags = 0;
-    if (pieces == 1) {
-        flags = token_flags(first, p, threadIdx.x * 8);
-        ln_load<NT, PER>(row, E + (size_t)pl.token * H, g, H);
-    }
+    ln_load<NT, PER>(row, E + (size_t)pl.token * H, g, H);
     float acc[PER][8] = {};
-    add_some_rows<NT, PER, _Float16, 1>(acc, 0, H, [&](int) { return (const _Float16 *)grad + (size_t)pl.position * H; });
-    add_rows<NT, PER, _Float16, 8>(acc, n - 1, H, [&](int r) { return (const _Float16 *)grad + (size_t)places[p + 1 + r].position * H; });
-    if (pieces > 1) {                                                // pieces begin at least RUN_PIECE places apart
-        ln_store<NT, PER>(acc, parts + (size_t)(p / RUN_PIECE) * H, H);
-        return;
-    }
-    count_tokens<NT>(first, p, flags, si);
-    ln_backward<NT, PER>(acc, row, H, eps, sd);
-    const int u = counted_tokens<NT>(si);
+    add_some_rows<NT, PER, _Float16, 1>(acc, 0, threadIdx.x * 8, H, [&](int) { return (const _Float16 *)grad + (size_t)pl.position * H; });
+    add_rows<NT, PER, _Float16, 8>(acc, pl.count - 1, threadIdx.x * 8, H,
+                                   [&](int r) { return (const _Float16 *)grad + (size_t)places[p + 1 + r].position * H; });
+    count_tokens<NT>(first, p, flags, sm.si);
+    ln_backward<NT, PER>(acc, row, H, eps, sm.sd);
+    const int u = counted_tokens<NT>(sm.si);
     ln_store<NT, PER>(acc, grads_out + (size_t)u * H, H);
     if (threadIdx.x == 0) tokens_out[u] = pl.token;
 }
 
-// the lists of several pieces: workgroup b looks for one that begins at places b * RUN_PIECE ..
+// The lists that went in pieces: workgroup s looks for one that begins at places s RUN_PIECE ..  (Joined in the launch before, by the
+// workgroup that is done last with a list: 34 us there instead of 20 + 5 here, the eight L2 caches have to be brought in line.)
 template <int NT, int PER>
 __global__ void __launch_bounds__(NT) k_embed_backward_join(int M, int H, const __half *__restrict__ E, const __half *__restrict__ g, float eps,
                                                             const Place *__restrict__ places, const uint8_t *__restrict__ first,
@@ -588,21 +620,14 @@ __global__ void __launch_bounds__(NT) k_embed_backward_join(int M, int H, const 
                                                             float *__restrict__ grads_out) {
     __shared__ double sd[NT / 64][4];
     __shared__ int si[NT / 64];
-    const int lane = threadIdx.x & 63, q = blockIdx.x * RUN_PIECE + lane;
-    bool begins = false;
-    if (lane < RUN_PIECE && q < M) {
-        const Place pl = places[q];
-        begins = pl.before == 0 && run_pieces(pl.count) > 1;         // at most one does
-    }
-    const unsigned long long who = __ballot(begins);                 // (every wave for itself)
-    if (!who) return;
-    const int p = blockIdx.x * RUN_PIECE + __builtin_ctzll(who);
+    const int p = find_place(places, blockIdx.x, M, [](const Place &pl) { return pl.before == 0 && run_pieces(pl.count) > 0; });
+    if (p < 0) return;
     const Place pl = places[p];
     LnRow<PER> row;
     const uint64_t flags = token_flags(first, p, threadIdx.x * 8);
     ln_load<NT, PER>(row, E + (size_t)pl.token * H, g, H);
     float acc[PER][8] = {};
-    add_rows<NT, PER, float, 4>(acc, run_pieces(pl.count), H, [&](int r) { return parts + (size_t)(p / RUN_PIECE + r) * H; });
+    add_rows<NT, PER, float, 4>(acc, run_pieces(pl.count), threadIdx.x * 8, H, [&](int r) { return parts + (size_t)(p / RUN_PIECE + r) * H; });
     count_tokens<NT>(first, p, flags, si);
     ln_backward<NT, PER>(acc, row, H, eps, sd);
     const int u = counted_tokens<NT>(si);
@@ -614,9 +639,9 @@ template <int NT, int PER>
 void embed_backward(const __half *grad, int M, int H, const __half *E, const __half *g, float eps,
                     const Place *places, const uint8_t *first, float *parts, int32_t *tokens_out, float *grads_out, int32_t *count_out,
                     hipStream_t st) {
-    k_embed_backward<NT, PER><<<M, NT, 0, st>>>(grad, M, H, E, g, eps, places, first, parts, tokens_out, grads_out, count_out);
-    if (M >= 2 * RUN_PIECE)
-        k_embed_backward_join<NT, PER><<<(M + RUN_PIECE - 1) / RUN_PIECE, NT, 0, st>>>(M, H, E, g, eps, places, first, parts, tokens_out, grads_out);
+    const int runs = M < RUN_PIECE ? 0 : (M + RUN_PIECE - 1) / RUN_PIECE, pieces = runs * ((H + PIECE_COLUMNS - 1) / PIECE_COLUMNS);
+    k_embed_backward<NT, PER><<<pieces + M, NT, 0, st>>>(grad, M, H, E, g, eps, places, first, pieces, parts, tokens_out, grads_out, count_out);
+    if (runs) k_embed_backward_join<NT, PER><<<runs, NT, 0, st>>>(M, H, E, g, eps, places, first, parts, tokens_out, grads_out);
 }
 
 int check_call(const petals_client_config &cfg, int32_t M) {

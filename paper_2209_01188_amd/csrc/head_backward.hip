@@ -242,7 +242,7 @@ __global__ void __launch_bounds__(NT) k_head_finish(const float *__restrict__ pa
     LnRow<PER> lr;
     ln_load<NT, PER>(lr, x + (size_t)t * H, g, H);
     float acc[PER][8] = {};
-    add_rows<NT, PER, float, 8 / PER>(acc, splits, H, [&](int s) { return part + ((size_t)s * M + t) * H; });
+    add_rows<NT, PER, float, 8 / PER>(acc, splits, threadIdx.x * 8, H, [&](int s) { return part + ((size_t)s * M + t) * H; });
     ln_backward<NT, PER>(acc, lr, H, eps, sm);
     ln_store<NT, PER>(acc, out + (size_t)t * H, H);
 }

@@ -94,16 +94,16 @@ __device__ __forceinline__ void ln_store(const float (&acc)[PER][8], __half *__r
     }
 }
 
-// acc += rows r0 .. r0 + N - 1 in order, row(r) the address of row r, all N on their way at once
+// acc += columns k0 + 8 NT i .. + 8 (below H) of rows r0 .. r0 + N - 1 in order, row(r) the address of row r, all N on their way at once
 template <int NT, int PER, typename T, int N, typename F>
-__device__ __forceinline__ void add_some_rows(float (&acc)[PER][8], int r0, int H, F row) {
+__device__ __forceinline__ void add_some_rows(float (&acc)[PER][8], int r0, int k0, int H, F row) {
     typedef T v8 __attribute__((ext_vector_type(8), aligned(sizeof(T))));
     const T *from[N];
 #pragma unroll
     for (int u = 0; u < N; u++) from[u] = row(r0 + u);
 #pragma unroll
     for (int i = 0; i < PER; i++) {
-        const int k = (threadIdx.x + i * NT) * 8;
+        const int k = k0 + i * NT * 8;
         if (k >= H) continue;
         v8 f[N];
 #pragma unroll
@@ -116,10 +116,10 @@ __device__ __forceinline__ void add_some_rows(float (&acc)[PER][8], int r0, int 
 }
 // rows 0 .. n - 1, AHEAD (a power of two) at a time
 template <int NT, int PER, typename T, int AHEAD, typename F>
-__device__ __forceinline__ void add_rows(float (&acc)[PER][8], int n, int H, F row) {
+__device__ __forceinline__ void add_rows(float (&acc)[PER][8], int n, int k0, int H, F row) {
     int r = 0;
-    for (; r + AHEAD <= n; r += AHEAD) add_some_rows<NT, PER, T, AHEAD>(acc, r, H, row);
+    for (; r + AHEAD <= n; r += AHEAD) add_some_rows<NT, PER, T, AHEAD>(acc, r, k0, H, row);
     if constexpr (AHEAD > 1) {
-        if (r < n) add_rows<NT, PER, T, AHEAD / 2>(acc, n - r, H, [&](int q) { return row(r + q); });
+        if (r < n) add_rows<NT, PER, T, AHEAD / 2>(acc, n - r, k0, H, [&](int q) { return row(r + q); });
     }
 }
