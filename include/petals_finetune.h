@@ -97,7 +97,7 @@ int petals_client_lm_head_backward(petals_client *client, void *dev_store, const
  *   tokens_out        dev int32 [M]: the different tokens in ascending order
  *   grads_out         dev fp32 [M, H]: row i = the gradient of embeddings[tokens_out[i]], through the LayerNorm behind the lookup
  *   count_out         dev int32 [1]: how many there are; entries of the two outputs from there on are left as they were
- * The rows of a token are summed in fp32 in an order that depends on the token's number of positions alone, then go through the
+ * The rows of a token are summed in fp32 in an order that depends on H and on their number alone, then go through the
  * derivative of the LayerNorm once.  Outputs may not overlap the inputs.  M <= max_rows_per_call, else PETALS_ERR_CAPACITY.
  */
 int petals_client_embed_backward(petals_client *client, const int32_t *token_ids, const void *grad_hidden, int32_t M,

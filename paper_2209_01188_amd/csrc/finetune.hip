@@ -451,6 +451,10 @@ __global__ void __launch_bounds__(ROW_NT) k_distill(DistillIn d, int first2, int
 //
 // Places in token order by counting: place of position i = number of j with (token_j, j) < (token_i, i).  No order of
 // atomics enters, and a call of a few thousand positions is a few million comparisons.
+//
+// 4096 x 4096 with 1300 different tokens: places 7.5 us, sums and short lists 19.5, the long lists' tokens 5.5; its 65 MB (gradients
+// once, matrix rows, results) are 14 us at the rate of a copy.  Few rows (128 x 4096, 16 tokens: 12 us) wait for three launches, each
+// of which reads an address before it reads a row.
 struct __align__(16) Place {
     int position, token, before, count;      // a position and its token; how many earlier ones have the same, and how many in all
 };
@@ -530,8 +534,8 @@ __device__ __forceinline__ int find_place(const Place *__restrict__ places, int 
     return who ? s * RUN_PIECE + __builtin_ctzll(who) : -1;
 }
 
-// Number of different tokens before place p, over the workgroup: each thread's first flags (8 places; first is padded to that) asked
-// for early, then the waves' sums, and behind a barrier all of them.
+// Number of different tokens before place p, over the workgroup: each thread's first flags (8 places; the memory behind `first` reaches
+// to a multiple of that) asked for early, then the waves' sums, and behind a barrier all of them.
 __device__ __forceinline__ uint64_t token_flags(const uint8_t *__restrict__ first, int p, int q) {
     if (q >= p) return 0;
     const uint64_t w = *(const uint64_t *)(first + q);

@@ -1,5 +1,10 @@
 // Backward of the LM head: da = G E (G fp32 [M, V] the gradient of the logits, E fp16 [V, H] the embedding matrix where the
-// client keeps it), then the derivative of the final LayerNorm.
+// client keeps it), then the derivative of the final LayerNorm.  Three launches: G to fp16 tiles, the product in blocks with the
+// contraction split, the sums of the splits with the LayerNorm.
+//
+// 2048 x 250880 x 4096: 540 + 3340 to 3700 + 30 us (1140 to 1260 TFLOP/s in the product, by the clock that the card's power leaves;
+// an fp16 library product of this size alone 3360); 351 x 50257 x 2560: 22 + 105 + 12; 24 x 250880 x 14336: 14 + 1260 + 16, 5.7 TB/s
+// of E; 16 x 50257 x 1024: 6 + 18 + 7.
 #include <mutex>
 
 #include "../../include/petals_finetune.h"
@@ -20,7 +25,7 @@ typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));     // ro
 // mostly the label's, exactly.  lo (may be null): what the rounding left, in the same scale.
 // A wave per row and section, SKT k-tiles: it reads 1 KB of the row at a time (a row of an odd vocabulary begins anywhere; the
 // tiles' own 128 bytes of it would touch two lines each), takes the maximum, and drops its halves into LDS where the tiles lie;
-// from there they go out as whole tiles of 16 rows.  272 bytes from one group of 8 columns to the next, so that the 64 lanes'
+// from there they go out as whole tiles of 16 rows.  Bound by its bytes: 5.7 TB/s at 2048 x 250880.  272 bytes from one group of 8 columns to the next, so that the 64 lanes'
 // halves fall on different banks.
 constexpr int PACK_GROUP = 16 * 16 + 16, PACK_TILE = 4 * PACK_GROUP;
 constexpr int head_section_kt(bool pair) { return pair ? 32 : 64; }
@@ -81,9 +86,12 @@ __global__ void __launch_bounds__(1024) k_head_pack(const float *__restrict__ G,
 
 // The product: output blocks of BM tokens x 256 columns, 8 waves of BM / 2 x 64, the contraction over the vocabulary split over
 // workgroups until every compute unit has one.  Token tiles and 32 rows x 512 bytes of E are copied to a ring of slots in LDS,
-// as many stages ahead as fit.  The contraction runs along E's columns in memory, so its operands are turned around: a lane reads 4 columns
+// NSLOT - 1 stages ahead (rings of 5 and 6 slots, which fit as well: no gain).  Eight waves, because a wave has 256 registers in two to
+// a SIMD: four of 128 x 128 would read a third less of LDS, but did not keep their sums in registers.  The contraction runs along E's columns in memory, so its operands are turned around: a lane reads 4 columns
 // of 8 rows and makes of them, one byte permutation per word, the A operands of 4 products (product i has columns 4 a + i).
 // PAIR: the token tiles twice, G's values and what their rounding left; calls of up to 64 rows, which wait for E's bytes anyway.
+// Full blocks are bound by the matrix instructions (69 % of the cycles busy, at the 1.7 GHz that their power leaves) and close to it
+// by LDS (256 x 256: 1024 cycles of each to a stage); with one round of blocks (351 x 50257 x 2560, 192 x 256) a stage takes 790 ns.
 constexpr int NSLOT = 4;
 template <int BM, bool PAIR>
 __global__ void __launch_bounds__(512, 2) k_head_block(const __half *__restrict__ E, const __half *__restrict__ hi, const __half *__restrict__ lo,
