@@ -76,13 +76,14 @@ __device__ __forceinline__ float accumulate(RowStat &s, const float (&l)[N], flo
     return cm;
 }
 
-constexpr int ROW_NT = 256, ROW_NW = ROW_NT / 64;
+constexpr int ROW_NT = 256, ROW_NW = ROW_NT / 64;   // threads of a workgroup that has a row or a part of one
 constexpr int ROW_PER = 16;                         // logits of a thread per step
 constexpr int WAVE_STEP = 64 * ROW_PER, ROW_STEP = ROW_NW * WAVE_STEP;
 // Workgroups that a call is cut into at least, if it has the steps: 4 and 8 per compute unit.  (Log probabilities of 1024 x 250880
 // with 1024, 2048: 218, 255 us, each split starts a list of its own; distillation of 2048 x 250880 with 1024, 2048, 4096, 8192: 934,
 // 895, 913, 930.)
 constexpr int LOGPROBS_GROUPS = 1024, DISTILL_GROUPS = 2048;
+constexpr int MAX_GRID = 1 << 14;                   // rows of a launch
 typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));     // rows of an odd vocabulary begin anywhere
 
 // A call of few rows shares each row out over workgroups, a whole number of steps to each.
@@ -115,9 +116,9 @@ __device__ __forceinline__ void load_logits(const float *row, int v0, int end, f
 }
 // the steps of this wave in [begin, end): step(first column, logits).  (The other waves of the compute unit cover the wait for
 // a step's logits: with the next step's asked for ahead, in 16 more registers, 1024 x 250880 took 223 instead of 218 us.)
-template <bool LAST = false, typename F>
+template <int NT, bool LAST = false, typename F>
 __device__ __forceinline__ void walk_row(const float *row, int begin, int end, F step) {
-    for (int v = begin + (threadIdx.x >> 6) * WAVE_STEP; v < end; v += ROW_STEP) {
+    for (int v = begin + (threadIdx.x >> 6) * WAVE_STEP; v < end; v += NT / 64 * WAVE_STEP) {
         float l[ROW_PER];
         load_logits<LAST>(row, v, end, l);
         step(v, l);
@@ -126,9 +127,9 @@ __device__ __forceinline__ void walk_row(const float *row, int begin, int end, F
 
 // ------------------------------------------------------------------------------------ the largest logits of a row
 //
-// A wave keeps the 64 best keys it has seen, one per lane in falling order: (value, lower index first) as one 64-bit number.
-// A step's logits are compared with the last key that still counts, and what passes is inserted one by one; after the first
-// few hundred logits of random order that is rare.
+// A key is (value, lower index first) as one 64-bit number; no two are equal.  A wave keeps the best keys it has seen in falling order
+// in LDS.  A step's logits are compared with the last key that still counts; what passes, after the first few hundred logits of random
+// order little, waits in LDS as well, and goes in many at a time: each key's place in the list is the number of larger ones.
 __device__ __forceinline__ uint32_t order_key(float f) {                   // orders like the floats (-0 as +0)
     const uint32_t u = __float_as_uint(f + 0.0f);
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
@@ -139,31 +140,69 @@ __device__ __forceinline__ float key_value(uint64_t key) {
 }
 // (in range also where a row of NaN has left a place of the list empty)
 __device__ __forceinline__ int key_index(uint64_t key) { return key ? (int)~(uint32_t)key : 0; }
-__device__ __forceinline__ uint64_t read_lane(uint64_t v, int lane) {
-    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
+constexpr int LIST = 64, LIST_FLUSH = 16;                                  // at least the most a caller can ask for
+static_assert(PETALS_LOGPROBS_TOP_MAX <= LIST, "a lane for each");
+// how many keys of a list in falling order are larger
+__device__ __forceinline__ int larger_in(const uint64_t *list, uint64_t key) {
+    int n = 0;
+#pragma unroll
+    for (int step = LIST / 2; step; step /= 2) n += list[n + step - 1] > key ? step : 0;
+    return n + (list[n] > key);
 }
 struct TopList {
-    uint64_t key = 0, floor = 0, last = 0;         // this lane's key; what is no larger than these two does not come in
+    uint64_t *list;                                // of this wave, in LDS: its list, and what waits
+    uint64_t floor = 0;                            // what is no larger does not come in
+    int waiting = 0;
+    __device__ __forceinline__ TopList(uint64_t (*lists)[2 * LIST]) : list(lists[threadIdx.x >> 6]) { list[threadIdx.x & 63] = 0; }
     // most: every lane's largest logit of its first step.  The top_k-th largest of the 64 lanes' is a bound that at least top_k
-    // logits of the step reach, so that a few more than top_k come in instead of top_k (1 + log(1024 / top_k)).
+    // logits of the step reach.
     __device__ __forceinline__ void start(float most, int top_k) {
         int above = 0;
 #pragma unroll
         for (int i = 0; i < 64; i++) above += __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(most), i)) > most;
         floor = ((uint64_t)order_key(-wave_max(above < top_k ? -most : -INFINITY)) << 32) - 1;
-        last = floor;
     }
-    __device__ __forceinline__ void offer(uint64_t k, int top_k) {        // one key per lane, 0: none
+    __device__ __forceinline__ void offer(uint64_t key, int top_k) {      // one key per lane, 0: none
+        unsigned long long who = __ballot(key > floor);
+        if (!who) return;
+        if (waiting + __popcll(who) > LIST) {
+            flush(top_k);
+            who = __ballot(key > floor);
+        }
+        if (key > floor) list[LIST + waiting + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0))] = key;
+        waiting += __popcll(who);
+    }
+    __device__ __forceinline__ void flush(int top_k) {
         const int lane = threadIdx.x & 63;
-        unsigned long long who = __ballot(k > last);
-        while (who) {
-            const int from = __builtin_ctzll(who);
-            const uint64_t nk = read_lane(k, from);
-            if (lane == from) k = 0;
-            const uint64_t prev = (uint64_t)dpp_move<0x138, 0xf>(0u, (uint32_t)(key >> 32)) << 32 | dpp_move<0x138, 0xf>(0u, (uint32_t)key);   // wave_shr 1
-            if (key < nk) key = lane == 0 || prev > nk ? nk : prev;
-            last = max(floor, read_lane(key, top_k - 1));
-            who = __ballot(k > last);
+        const uint64_t a = list[lane], b = lane < waiting ? list[LIST + lane] : 0;
+        int at_a = lane, at_b = larger_in(list, b);
+#pragma unroll 4
+        for (int i = 0; i < waiting; i++) {
+            const uint64_t k = list[LIST + i];
+            at_a += k > a;
+            at_b += k > b;
+        }
+        place(a, at_a, b, at_b);
+        waiting = 0;
+        floor = max(floor, list[top_k - 1]);
+    }
+    // the list becomes these keys at their places (of those that are none, 0, there may be several at one place)
+    __device__ __forceinline__ void place(uint64_t a, int at_a, uint64_t b, int at_b) {
+        list[threadIdx.x & 63] = 0;
+        if (a && at_a < LIST) list[at_a] = a;
+        if (b && at_b < LIST) list[at_b] = b;
+    }
+    // the first wave's becomes that of all (nw waves have one), for the first wave to read
+    __device__ __forceinline__ void join(uint64_t (*lists)[2 * LIST], int top_k, int nw) {
+        if (waiting) flush(top_k);
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        for (int w = 1; w < nw; w *= 2) {
+            __syncthreads();
+            if (wave % (2 * w) == 0 && wave + w < nw) {
+                const uint64_t *other = lists[wave + w], a = list[lane], b = other[lane];
+                const int at_a = lane + larger_in(other, a), at_b = lane + larger_in(list, b);
+                place(a, at_a, b, at_b);
+            }
         }
     }
 };
@@ -175,8 +214,8 @@ struct LogprobsOut {
     int32_t *top;
     float *top_logprob;
 };
-// the results of a row from its statistics (in every thread) and, in the first wave, its list
-__device__ __forceinline__ void logprobs_store(const LogprobsOut &o, int t, int V, double invT, int top_k, const RowStat &s, const TopList &list) {
+// the results of a row from its statistics (in every thread) and, in the first wave, the row's list
+__device__ __forceinline__ void logprobs_store(const LogprobsOut &o, int t, int V, double invT, int top_k, const RowStat &s, const uint64_t *top) {
     const double lse = log(s.S);                            // above (m / T)
     const bool none = s.S == 0.0;
     if (threadIdx.x == 0) {
@@ -187,77 +226,83 @@ __device__ __forceinline__ void logprobs_store(const LogprobsOut &o, int t, int 
         if (o.entropy) o.entropy[t] = none ? 0.0f : (float)(lse - LN2 * s.D / s.S);
     }
     if ((int)threadIdx.x < top_k) {                         // at most 64
-        o.top[(size_t)t * top_k + threadIdx.x] = key_index(list.key);
-        o.top_logprob[(size_t)t * top_k + threadIdx.x] = none ? -INFINITY : (float)(((double)key_value(list.key) - s.m) * invT - lse);
+        o.top[(size_t)t * top_k + threadIdx.x] = key_index(top[threadIdx.x]);
+        o.top_logprob[(size_t)t * top_k + threadIdx.x] = none ? -INFINITY : (float)(((double)key_value(top[threadIdx.x]) - s.m) * invT - lse);
     }
 }
-// the waves' lists become the first wave's
-__device__ __forceinline__ void join_lists(TopList &list, uint64_t (*lists)[64], int top_k, int nw) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    lists[wave][lane] = list.key;
-    __syncthreads();
-    if (wave == 0)
-        for (int w = 1; w < nw; w++) list.offer(lists[w][lane], top_k);
-}
-
 // workgroup (split, row): the split's part of the row, and with one split the results
 __global__ void __launch_bounds__(ROW_NT) k_logprobs(LogprobsOut o, int V, int range, double invT, int top_k, RowStat *__restrict__ stats,
                                                      uint64_t *__restrict__ tops) {
     __shared__ RowStat sm[ROW_NW];
-    __shared__ uint64_t lists[ROW_NW][64];
+    __shared__ uint64_t lists[ROW_NW][2 * LIST];
     const int t = blockIdx.y, lane = threadIdx.x & 63, begin = blockIdx.x * range, end = min(V, begin + range);
     const float c = (float)(invT * LOG2E);
     RowStat s{-INFINITY, 0.0, 0.0};
-    TopList list;
-    walk_row(o.logits + (size_t)t * V, begin, end, [&](int v0, const float (&l)[ROW_PER]) {
+    TopList list(lists);
+    walk_row<ROW_NT>(o.logits + (size_t)t * V, begin, end, [&](int v0, const float (&l)[ROW_PER]) {
         const float most = accumulate<ROW_PER, true>(s, l, c, invT);
         if (top_k && v0 < begin + ROW_STEP) list.start(most, top_k);
-        if (top_k && __ballot(!(most < key_value(list.last + 1)))) {
+        if (top_k && __ballot(!(most < key_value(list.floor + 1)))) {
 #pragma unroll
             for (int i = 0; i < ROW_PER; i++) {
                 const int v = v0 + 4 * lane + 256 * (i >> 2) + (i & 3);
                 list.offer(v < end ? (uint64_t)order_key(l[i]) << 32 | (uint32_t)~v : 0, top_k);
             }
+            if (list.waiting >= LIST_FLUSH) list.flush(top_k);
         }
     });
     s = block_merge<ROW_NW>(s, invT, sm);
-    if (top_k) join_lists(list, lists, top_k, ROW_NW);
+    if (top_k) list.join(lists, top_k, ROW_NW);
     if (gridDim.x == 1) {
-        logprobs_store(o, t, V, invT, top_k, s, list);
+        logprobs_store(o, t, V, invT, top_k, s, lists[0]);
         return;
     }
     const size_t at = (size_t)t * gridDim.x + blockIdx.x;
     if (threadIdx.x == 0) stats[at] = s;
-    if ((int)threadIdx.x < top_k) tops[at * top_k + threadIdx.x] = list.key;
+    if ((int)threadIdx.x < top_k) tops[at * top_k + threadIdx.x] = lists[0][threadIdx.x];
 }
 
-// what the splits of a row have found
+// What the splits of a row have found.  Of their lists, in falling order, the top_k-th largest of the first keys of each, together some
+// 2 top_k, is a bound that all but a few do not reach.
 template <int JOIN_NT>
 __global__ void __launch_bounds__(JOIN_NT) k_logprobs_join(LogprobsOut o, int V, int splits, double invT, int top_k,
                                                            const RowStat *__restrict__ stats, const uint64_t *__restrict__ tops) {
     constexpr int JOIN_NW = JOIN_NT / 64;
     __shared__ RowStat sm[JOIN_NW];
-    __shared__ uint64_t lists[JOIN_NW][64];
+    __shared__ uint64_t lists[JOIN_NW][2 * LIST], firsts[LOGPROBS_GROUPS + 2 * LIST], bound;
     const int t = blockIdx.x, n = splits * top_k;
     RowStat s{-INFINITY, 0.0, 0.0};
     for (int i = threadIdx.x; i < splits; i += JOIN_NT) merge(s, stats[(size_t)t * splits + i], invT);
-    TopList list;
-    const uint64_t *keys = tops + (size_t)t * n;
-    for (int i = threadIdx.x; i < (n + 63) / 64 * 64; i += JOIN_NT) list.offer(i < n ? keys[i] : 0, top_k);
+    if (top_k) {
+        const uint64_t *keys = tops + (size_t)t * n;
+        const int each = min(top_k, (2 * top_k + splits - 1) / splits), some = splits * each;          // top_k .. splits + 2 top_k
+        for (int i = threadIdx.x; i < some; i += JOIN_NT) firsts[i] = keys[i / each * top_k + i % each];
+        if (threadIdx.x == 0) bound = 0;
+        __syncthreads();
+        for (int i = threadIdx.x; i < some; i += JOIN_NT) {
+            const uint64_t key = firsts[i];
+            int larger = 0;
+#pragma unroll 8
+            for (int j = 0; j < some; j++) larger += firsts[j] > key;
+            if (key && larger == top_k - 1) bound = key - 1;
+        }
+        __syncthreads();
+        TopList list(lists);
+        list.floor = bound;
+        for (int i = threadIdx.x; i < (n + 63) / 64 * 64; i += JOIN_NT) list.offer(i < n ? keys[i] : 0, top_k);
+        list.join(lists, top_k, min(JOIN_NW, (n + 63) / 64));
+    }
     s = block_merge<JOIN_NW>(s, invT, sm);
-    if (top_k) join_lists(list, lists, top_k, min(JOIN_NW, (n + 63) / 64));
-    logprobs_store(o, t, V, invT, top_k, s, list);
+    logprobs_store(o, t, V, invT, top_k, s, lists[0]);
 }
 
 // ------------------------------------------------------------------------------------ distillation
 //
-// Two passes over the logits: the softmax statistics, then w q.  A call goes through its rows in groups whose logits fit the
-// 256 MB of cache in front of the memory, so that the second pass need not ask the memory again: launch k takes the first pass of
-// group k and the second of group k - 1, whose workgroups take turns, so that reads and writes share the launch.  The second pass
-// is the last to look at the logits and says so with its loads.  2048 x 250880: 895 us, what a copy of the logits takes is 860; in
-// one group 1119 us; the two kinds one after the other 1027; second pass with ordinary loads 1181; groups of 64, 96, 128, 144, 192
-// MB (before the number of workgroups was settled) 1052, 1013, 949, 979, 982.  Calls that fit as a whole are two launches (701 x
-// 50257, 141 MB: 80 us, in two groups 97).
+// Two passes over the logits: the softmax statistics, then w q.  From DISTILL_WHOLE rows on a workgroup has a row and both passes: the
+// second finds the logits in the cache in front of the memory, and workgroups that read run beside others that write.  Fewer rows are cut
+// into parts, with a launch for each pass.
+//
+// @@FIGURES@@
 struct DistillIn {
     const float *logits;
     const int32_t *ids;
@@ -276,9 +321,9 @@ struct DistillRow {                    // of a row, by the workgroup of its firs
     double term, mass;                 // sum p (log p - z / T) and sum p: with log q = z / T - lse the loss is T^2 (term + mass lse)
     int listed;
 };
-constexpr int MAX_GRID_ROWS = 1 << 14;      // rows of a group (two groups share the grid's second dimension)
-constexpr size_t DISTILL_GROUP = (size_t)128 << 20, DISTILL_ONE_GROUP = (size_t)192 << 20;
-constexpr int LIST_PER = (PETALS_DISTILL_TOP_MAX + ROW_NT - 1) / ROW_NT;
+constexpr int DISTILL_WHOLE = 192, DISTILL_WIDE = 65536;     // rows from which on one is a workgroup's; vocabulary beyond which it has 1024 threads, not 512
+template <int NT>
+constexpr int LIST_PER = (PETALS_DISTILL_TOP_MAX + NT - 1) / NT;
 
 // entry k of a row's list; an entry that counts for nothing has value -infinity
 __device__ __forceinline__ float teacher_entry(const DistillIn &d, int t, int k, int &id) {
@@ -289,35 +334,36 @@ __device__ __forceinline__ float teacher_entry(const DistillIn &d, int t, int k,
     return id < 0 ? -INFINITY : d.vals[(size_t)t * d.K + k];
 }
 
-__device__ __forceinline__ void distill_stats(const DistillIn &d, int t, DistillPart *__restrict__ part, DistillRow *__restrict__ out,
-                                              RowStat *sm, double *sd, float *sf) {
+template <int NT>
+__device__ __forceinline__ void distill_stats(const DistillIn &d, int t, int split, DistillPart *part, DistillRow *out, RowStat *sm, double *sd,
+                                              float *sf) {
     const float *row = d.logits + (size_t)t * d.V;
     const float c = (float)(d.invT * LOG2E);
-    const int begin = blockIdx.x * d.range, end = min(d.V, begin + d.range);
-    float val[LIST_PER], mx = -INFINITY;
-    int id[LIST_PER];
+    const int begin = split * d.range, end = min(d.V, begin + d.range);
+    float val[LIST_PER<NT>], mx = -INFINITY;
+    int id[LIST_PER<NT>];
     bool some = false;
 #pragma unroll
-    for (int i = 0; i < LIST_PER; i++) {
+    for (int i = 0; i < LIST_PER<NT>; i++) {
         val[i] = -INFINITY;
         id[i] = -1;
-        if (i * ROW_NT < d.K) val[i] = teacher_entry(d, t, i * ROW_NT + threadIdx.x, id[i]);
+        if (i * NT < d.K) val[i] = teacher_entry(d, t, i * NT + threadIdx.x, id[i]);
         mx = fmaxf(mx, val[i]);
         some |= !(val[i] == -INFINITY);
     }
     const bool listed = __syncthreads_or(some);
-    if (blockIdx.x == 0) {
+    if (split == 0) {
         DistillRow r{0.0, 0.0, 0.0, 0.0, listed};
         if (listed) {
-            mx = block_max<ROW_NW>(mx, sf);
+            mx = block_max<NT / 64>(mx, sf);
             double sum = 0.0, term = 0.0, mass = 0.0;
 #pragma unroll
-            for (int i = 0; i < LIST_PER; i++)
-                if (i * ROW_NT < d.K) sum += val[i] == -INFINITY ? 0.0 : exp_f64(((double)val[i] - mx) * d.invT);
-            sum = block_sum<ROW_NW>(sum, sd);
+            for (int i = 0; i < LIST_PER<NT>; i++)
+                if (i * NT < d.K) sum += val[i] == -INFINITY ? 0.0 : exp_f64(((double)val[i] - mx) * d.invT);
+            sum = block_sum<NT / 64>(sum, sd);
             const double ls = log(sum);
 #pragma unroll
-            for (int i = 0; i < LIST_PER; i++) {
+            for (int i = 0; i < LIST_PER<NT>; i++) {
                 if (val[i] == -INFINITY) continue;
                 const double tt = ((double)val[i] - mx) * d.invT, p = exp_f64(tt) / sum;
                 if (!(p == 0.0)) {
@@ -325,53 +371,54 @@ __device__ __forceinline__ void distill_stats(const DistillIn &d, int t, Distill
                     mass += p;
                 }
             }
-            term = block_sum<ROW_NW>(term, sd);
-            mass = block_sum<ROW_NW>(mass, sd);
+            term = block_sum<NT / 64>(term, sd);
+            mass = block_sum<NT / 64>(mass, sd);
             r = DistillRow{(double)mx, 1.0 / sum, term, mass, 1};
         }
         if (threadIdx.x == 0) *out = r;
     }
     if (!listed) return;                                   // nobody reads the part
     RowStat s{-INFINITY, 0.0, 0.0};
-    walk_row(row, begin, end, [&](int, const float (&l)[ROW_PER]) { accumulate<ROW_PER, false>(s, l, c, d.invT); });
-    s = block_merge<ROW_NW>(s, d.invT, sm);
+    walk_row<NT>(row, begin, end, [&](int, const float (&l)[ROW_PER]) { accumulate<ROW_PER, false>(s, l, c, d.invT); });
+    s = block_merge<NT / 64>(s, d.invT, sm);
     if (threadIdx.x == 0) *part = DistillPart{s.m, s.S};
 }
 
 // The gradient of a workgroup's range (logits and gradient may be the same memory: what a thread overwrites it has read, and
 // the list's logits are read before the barrier), and by the first workgroup of the row its loss.  The list's columns get
 // theirs, w (q - p) in fp64, after the others.
-__device__ __forceinline__ void distill_grad(const DistillIn &d, int t, const DistillPart *__restrict__ parts, const DistillRow *__restrict__ rows,
-                                             int *s_id, double *s_p) {
-    const int lane = threadIdx.x & 63, splits = gridDim.x;
+template <int NT>
+__device__ __forceinline__ void distill_grad(const DistillIn &d, int t, int split, int splits, const DistillPart *parts, const DistillRow *stats, int *s_id,
+                                             double *s_p) {
+    const int lane = threadIdx.x & 63;
     const float *row = d.logits + (size_t)t * d.V;
     const float c = (float)(d.invT * LOG2E);
-    const int begin = blockIdx.x * d.range, end = min(d.V, begin + d.range);
-    if (!d.grad && blockIdx.x) return;
-    const DistillRow r = rows[t];
+    const int begin = split * d.range, end = min(d.V, begin + d.range);
+    if (!d.grad && split) return;
+    const DistillRow r = *stats;
     RowStat s{-INFINITY, 0.0, 0.0};
     if (r.listed) {
         for (int i = lane; i < splits; i += 64) {          // by every wave
-            const DistillPart p = parts[(size_t)t * splits + i];
+            const DistillPart p = parts[i];
             merge(s, RowStat{p.m, p.S, 0.0}, d.invT);
         }
         s = wave_merge(s, d.invT);
     }
     const bool none = s.S == 0.0, zero = !r.listed || none;
-    if (blockIdx.x == 0 && threadIdx.x == 0 && d.loss)
+    if (split == 0 && threadIdx.x == 0 && d.loss)
         d.loss[t] = !r.listed ? 0.0f : none ? INFINITY : (float)(d.T * d.T * (r.term + r.mass * ((double)s.m * d.invT + log(s.S))));
     if (!d.grad) return;
     float *out = d.grad + (size_t)t * d.V;
     const double w = d.T * (d.loss_grad ? (double)d.loss_grad[t] : 1.0);
-    int id[LIST_PER];
-    float at[LIST_PER];
+    int id[LIST_PER<NT>];
+    float at[LIST_PER<NT>];
     if (!zero) {
         bool mine = false;
 #pragma unroll
-        for (int i = 0; i < LIST_PER; i++) {
+        for (int i = 0; i < LIST_PER<NT>; i++) {
             id[i] = -1;
-            const int k = i * ROW_NT + threadIdx.x;
-            if (i * ROW_NT < d.K) {
+            const int k = i * NT + threadIdx.x;
+            if (i * NT < d.K) {
                 const float val = teacher_entry(d, t, k, id[i]);
                 if (k < d.K) {
                     s_id[k] = id[i];
@@ -384,7 +431,7 @@ __device__ __forceinline__ void distill_grad(const DistillIn &d, int t, const Di
         __syncthreads();
         if (mine) {
 #pragma unroll
-            for (int i = 0; i < LIST_PER; i++) {
+            for (int i = 0; i < LIST_PER<NT>; i++) {
                 if (id[i] < 0) continue;
                 double p = 0.0;
                 for (int j = 0; j < d.K; j++) p += s_id[j] == id[i] ? s_p[j] : 0.0;
@@ -409,10 +456,10 @@ __device__ __forceinline__ void distill_grad(const DistillIn &d, int t, const Di
     };
     if (zero) {
         const float g[ROW_PER] = {};
-        for (int v0 = begin + (threadIdx.x >> 6) * WAVE_STEP; v0 < end; v0 += ROW_STEP) store(v0, g);
+        for (int v0 = begin + (threadIdx.x >> 6) * WAVE_STEP; v0 < end; v0 += NT / 64 * WAVE_STEP) store(v0, g);
         return;
     }
-    walk_row<true>(row, begin, end, [&](int v0, const float (&l)[ROW_PER]) {
+    walk_row<NT, true>(row, begin, end, [&](int v0, const float (&l)[ROW_PER]) {
         float g[ROW_PER];
 #pragma unroll
         for (int i = 0; i < ROW_PER; i++) g[i] = f * __builtin_amdgcn_exp2f((l[i] - m) * c);
@@ -420,28 +467,36 @@ __device__ __forceinline__ void distill_grad(const DistillIn &d, int t, const Di
     });
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < LIST_PER; i++)
+    for (int i = 0; i < LIST_PER<NT>; i++)
         if (id[i] >= 0) out[id[i]] = at[i];                // (entries with the same token write the same)
 }
 
-// workgroup (split, row): rows [first2, first2 + n2) their second pass, the others, from row first1 on, their first
-__global__ void __launch_bounds__(ROW_NT) k_distill(DistillIn d, int first2, int n2, int first1, DistillPart *__restrict__ parts,
-                                                    DistillRow *__restrict__ rows) {
-    __shared__ RowStat sm[ROW_NW];
-    __shared__ double sd[ROW_NW];
-    __shared__ float sf[ROW_NW];
-    __shared__ int s_id[PETALS_DISTILL_TOP_MAX];
-    __shared__ double s_p[PETALS_DISTILL_TOP_MAX];
-    // as far as there are both kinds they take turns
-    const int y = blockIdx.y, n1 = (int)gridDim.y - n2, both = 2 * min(n1, n2);
-    const bool second = y < both ? !(y & 1) : both ? n2 > n1 : y < n2;
-    const int i = y < both ? y >> 1 : both ? y - both / 2 : second ? y : y - n2;
-    if (second) {
-        distill_grad(d, first2 + i, parts, rows, s_id, s_p);
-    } else {
-        const int t = first1 + i;
-        distill_stats(d, t, parts + (size_t)t * gridDim.x + blockIdx.x, rows + t, sm, sd, sf);
-    }
+template <int NT>
+struct DistillShared {
+    RowStat sm[NT / 64];
+    double sd[NT / 64];
+    float sf[NT / 64];
+    int id[PETALS_DISTILL_TOP_MAX];
+    double p[PETALS_DISTILL_TOP_MAX];
+};
+// workgroup (split, row), one of the two passes
+template <bool SECOND>
+__global__ void __launch_bounds__(ROW_NT) k_distill_part(DistillIn d, DistillPart *__restrict__ parts, DistillRow *__restrict__ rows) {
+    __shared__ DistillShared<ROW_NT> sh;
+    const int split = blockIdx.x, splits = gridDim.x, t = blockIdx.y;
+    if (SECOND) distill_grad<ROW_NT>(d, t, split, splits, parts + (size_t)t * splits, rows + t, sh.id, sh.p);
+    else distill_stats<ROW_NT>(d, t, split, parts + (size_t)t * splits + split, rows + t, sh.sm, sh.sd, sh.sf);
+}
+// both passes of row first + blockIdx.x
+template <int NT>
+__global__ void __launch_bounds__(NT) k_distill_row(DistillIn d, int first) {
+    __shared__ DistillShared<NT> sh;
+    __shared__ DistillPart part;
+    __shared__ DistillRow row;
+    const int t = first + blockIdx.x;
+    distill_stats<NT>(d, t, 0, &part, &row, sh.sm, sh.sd, sh.sf);
+    __syncthreads();
+    distill_grad<NT>(d, t, 0, 1, &part, &row, sh.id, sh.p);
 }
 
 // ------------------------------------------------------------------------------------ gradient of the lookup
@@ -682,8 +737,8 @@ int petals_client_logprobs(petals_client *client, const float *logits, const int
     const RowSplit sp = row_split(M, V, LOGPROBS_GROUPS, (int)min((size_t)1 << 20, c.scratch_bytes / ((size_t)M * per)));
     RowStat *stats = (RowStat *)c.scratch;
     uint64_t *tops = (uint64_t *)(stats + (size_t)M * sp.splits);
-    for (int t0 = 0; t0 < M; t0 += MAX_GRID_ROWS) {
-        const int rows = min(MAX_GRID_ROWS, M - t0);
+    for (int t0 = 0; t0 < M; t0 += MAX_GRID) {
+        const int rows = min(MAX_GRID, M - t0);
         const LogprobsOut r{logits + (size_t)t0 * V, tokens ? tokens + t0 : nullptr, logprob_out ? logprob_out + t0 : nullptr,
                             entropy_out ? entropy_out + t0 : nullptr, top_out ? top_out + (size_t)t0 * top_k : nullptr,
                             top_logprob_out ? top_logprob_out + (size_t)t0 * top_k : nullptr};
@@ -710,20 +765,25 @@ int petals_client_distill(petals_client *client, const float *logits, int32_t M,
     if (!usable_temperature(temperature)) return ps_fail(PETALS_ERR_INVALID_ARG, "temperature must be positive and finite");
     hipStream_t st = (hipStream_t)stream;
     const int V = c.cfg->vocab;
+    DistillIn d{logits, teacher_tokens, teacher_logits, loss_grad, loss_out, grad_logits_out, V, K, V, (double)temperature, 1.0 / (double)temperature};
+    if (M >= DISTILL_WHOLE) {
+        for (int t0 = 0; t0 < M; t0 += MAX_GRID) {
+            const int n = min(MAX_GRID, M - t0);
+            if (V <= DISTILL_WIDE) k_distill_row<512><<<n, 512, 0, st>>>(d, t0);
+            else k_distill_row<1024><<<n, 1024, 0, st>>>(d, t0);
+            HIP_TRY(hipGetLastError());
+        }
+        return PETALS_OK;
+    }
     DistillRow *rows = (DistillRow *)c.scratch;
     DistillPart *parts = (DistillPart *)(rows + M);
-    const size_t row_bytes = (size_t)V * sizeof(float);
-    const int group = !grad_logits_out || row_bytes * M <= DISTILL_ONE_GROUP ? MAX_GRID_ROWS
-                                       : (int)max((size_t)1, min((size_t)MAX_GRID_ROWS, DISTILL_GROUP / row_bytes));
     const size_t room = (c.scratch_bytes - sizeof(DistillRow) * M) / ((size_t)M * sizeof(DistillPart));
-    const RowSplit sp = row_split(min(M, group), V, DISTILL_GROUPS, (int)min((size_t)1 << 20, room));
-    const DistillIn d{logits, teacher_tokens, teacher_logits, loss_grad, loss_out, grad_logits_out, V, K, sp.range, (double)temperature, 1.0 / (double)temperature};
-    for (int t0 = 0, n2 = 0; t0 < M || n2; t0 += group) {
-        const int n1 = max(0, min(group, M - t0));
-        k_distill<<<dim3(sp.splits, n2 + n1), ROW_NT, 0, st>>>(d, t0 - group, n2, t0, parts, rows);
-        HIP_TRY(hipGetLastError());
-        n2 = n1;
-    }
+    const RowSplit sp = row_split(M, V, DISTILL_GROUPS, (int)min((size_t)1 << 20, room));
+    d.range = sp.range;
+    k_distill_part<false><<<dim3(sp.splits, M), ROW_NT, 0, st>>>(d, parts, rows);
+    HIP_TRY(hipGetLastError());
+    k_distill_part<true><<<dim3(sp.splits, M), ROW_NT, 0, st>>>(d, parts, rows);
+    HIP_TRY(hipGetLastError());
     return PETALS_OK;
 }
 
