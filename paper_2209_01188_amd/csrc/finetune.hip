@@ -18,8 +18,8 @@ namespace {
 // well); the sums are fp64, so that S - 1, what is left beside the largest token, keeps its digits where that token has
 // nearly everything: log S and -D / S are the two parts of the entropy, both >= 0, and nothing cancels between them.
 //
-// Bound by the bytes of the logits where there are many rows: 1024 x 250880 with the 20 best of each in 199 us, 5.2 TB/s (a copy
-// within the memory reaches 4.8); with few rows by the latency of two launches, 1 x 250880 in 12 us.
+// Bound by the bytes of the logits where there are many rows: 1024 x 250880 with the 20 best of each in 194 us, 5.3 TB/s (a copy
+// within the memory reaches 4.8); with few rows by the latency of two launches, 1 x 250880 in 13 us with 5 of them, in 20 with 50.
 constexpr double LN2 = 0.69314718055994530942, LOG2E = 1.4426950408889634074;
 
 struct RowStat {
@@ -80,8 +80,7 @@ constexpr int ROW_NT = 256, ROW_NW = ROW_NT / 64;   // threads of a workgroup th
 constexpr int ROW_PER = 16;                         // logits of a thread per step
 constexpr int WAVE_STEP = 64 * ROW_PER, ROW_STEP = ROW_NW * WAVE_STEP;
 // Workgroups that a call is cut into at least, if it has the steps: 4 and 8 per compute unit.  (Log probabilities of 1024 x 250880
-// with 1024, 2048: 218, 255 us, each split starts a list of its own; distillation of 2048 x 250880 with 1024, 2048, 4096, 8192: 934,
-// 895, 913, 930.)
+// with 1024, 1536: 188, 205 us, each split starts a list of its own.)
 constexpr int LOGPROBS_GROUPS = 1024, DISTILL_GROUPS = 2048;
 constexpr int MAX_GRID = 1 << 14;                   // rows of a launch
 typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));     // rows of an odd vocabulary begin anywhere
@@ -129,7 +128,9 @@ __device__ __forceinline__ void walk_row(const float *row, int begin, int end, F
 //
 // A key is (value, lower index first) as one 64-bit number; no two are equal.  A wave keeps the best keys it has seen in falling order
 // in LDS.  A step's logits are compared with the last key that still counts; what passes, after the first few hundred logits of random
-// order little, waits in LDS as well, and goes in many at a time: each key's place in the list is the number of larger ones.
+// order little, waits in LDS as well, and goes in many at a time: each key's place in the list is the number of larger ones.  (Inserted
+// one by one, 120 cycles each: the 50 best of 1 x 250880 54 us instead of 20, of 300 x 50257 87 instead of 45, of 2048 x 250880 456
+// instead of 405; of the 5 best of 1 x 250880 11.5 instead of 13.)
 __device__ __forceinline__ uint32_t order_key(float f) {                   // orders like the floats (-0 as +0)
     const uint32_t u = __float_as_uint(f + 0.0f);
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
@@ -302,7 +303,9 @@ __global__ void __launch_bounds__(JOIN_NT) k_logprobs_join(LogprobsOut o, int V,
 // second finds the logits in the cache in front of the memory, and workgroups that read run beside others that write.  Fewer rows are cut
 // into parts, with a launch for each pass.
 //
-// @@FIGURES@@
+// Bound by the memory: 2048 x 250880 in 871 us (a copy of the logits takes 862), 701 x 50257 in 74 (59).  Rows as a whole against parts with
+// a launch for each pass: 64 x 250880 54 and 37 us, 128 67 and 68, 191 94 and 100; 2048 x 50257 196 and 303, 300 x 50257 39 and 44.
+// 512 against 1024 threads to a row: 300 x 20000 20 and 25 us, 701 x 50257 71 and 72, 701 x 100003 140 and 133, 2048 x 250880 1086 and 955.
 struct DistillIn {
     const float *logits;
     const int32_t *ids;
