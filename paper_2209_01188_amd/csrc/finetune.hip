@@ -697,13 +697,100 @@ __global__ void __launch_bounds__(NT) k_embed_backward_join(int M, int H, const 
     if (threadIdx.x == 0) tokens_out[u] = pl.token;
 }
 
+// A call of few positions in one launch: workgroup i has the token of position i if that is its first.  Against the launches above, 16 tokens
+// in turn: 128 x 1024 6.9 us instead of 8.9, 128 x 4096 7.1 instead of 9.8; 31 different ones of 14336 7.9 instead of 10.2.  One compute unit
+// reads some 65 GB/s, so the limit is where a single token costs some 5 us more than in pieces (128 x 4096 16 and 11); 256 x 1024 9 and 9, with
+// a single token 21 and 11.
+constexpr int FEW = 128;              // positions at most
+constexpr size_t FEW_VALUES = 512 << 10;
 template <int NT, int PER>
-void embed_backward(const __half *grad, int M, int H, const __half *E, const __half *g, float eps,
-                    const Place *places, const uint8_t *first, float *parts, int32_t *tokens_out, float *grads_out, int32_t *count_out,
-                    hipStream_t st) {
-    const int runs = M < RUN_PIECE ? 0 : (M + RUN_PIECE - 1) / RUN_PIECE, pieces = runs * ((H + PIECE_COLUMNS - 1) / PIECE_COLUMNS);
-    k_embed_backward<NT, PER><<<pieces + M, NT, 0, st>>>(grad, M, H, E, g, eps, places, first, pieces, parts, tokens_out, grads_out, count_out);
-    if (runs) k_embed_backward_join<NT, PER><<<runs, NT, 0, st>>>(M, H, E, g, eps, places, first, parts, tokens_out, grads_out);
+__global__ void __launch_bounds__(NT) k_embed_backward_few(const int32_t *__restrict__ ids, const __half *__restrict__ grad, int M, int V, int H,
+                                                           const __half *__restrict__ E, const __half *__restrict__ g, float eps,
+                                                           int32_t *__restrict__ tokens_out, float *__restrict__ grads_out,
+                                                           int32_t *__restrict__ count_out) {
+    constexpr int GROUPS = NT / FEW;
+    __shared__ __align__(16) int token[FEW];
+    __shared__ int list[FEW], first[GROUPS][FEW], n_same[NT / 64], n_less[NT / 64], n_all[NT / 64];
+    __shared__ double sd[NT / 64][4];
+    const int i = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = threadIdx.x % FEW, group = threadIdx.x / FEW;
+    const int own = min(max(ids[i], 0), V - 1), mine = j < M ? min(max(ids[j], 0), V - 1) : 0x7fffffff;      // (no token)
+    LnRow<PER> row;
+    ln_load<NT, PER>(row, E + (size_t)own * H, g, H);
+    float acc[PER][8] = {};
+    add_some_rows<NT, PER, _Float16, 1>(acc, 0, threadIdx.x * 8, H, [&](int) { return (const _Float16 *)grad + (size_t)i * H; });
+    if (group == 0) token[j] = mine;
+    const unsigned long long same = __ballot(group == 0 && mine == own);
+    if (lane == 0) n_same[wave] = __popcll(same);
+    if (__syncthreads_or(mine == own && j < i)) return;
+    // the token's positions in order
+    int n = 0, before = 0;
+#pragma unroll
+    for (int w = 0; w < FEW / 64; w++) {
+        before += w < wave ? n_same[w] : 0;
+        n += n_same[w];
+    }
+    if (same >> lane & 1) list[before + __popcll(same & ((1ull << lane) - 1))] = j;
+    // the first position of token j, by a share of the positions
+    int f = FEW;
+    for (int q = (M - 1) / (4 * GROUPS) * GROUPS + group; q >= 0; q -= GROUPS) {
+        const v4i o = q * 4 < FEW ? *(const v4i *)(token + q * 4) : v4i{-1, -1, -1, -1};
+#pragma unroll
+        for (int e = 3; e >= 0; e--) f = o[e] == mine ? q * 4 + e : f;
+    }
+    first[group][j] = f;
+    __syncthreads();
+    for (int u = 0; u < GROUPS; u++) f = min(f, first[u][j]);
+    const bool is_first = group == 0 && j < M && f == j;
+    const unsigned long long all = __ballot(is_first), less = __ballot(is_first && mine < own);
+    if (lane == 0) {
+        n_all[wave] = __popcll(all);
+        n_less[wave] = __popcll(less);
+    }
+    add_rows<NT, PER, _Float16, 8>(acc, n - 1, threadIdx.x * 8, H, [&](int r) { return (const _Float16 *)grad + (size_t)list[r + 1] * H; });
+    ln_backward<NT, PER>(acc, row, H, eps, sd);                      // (with a barrier)
+    int u = 0, count = 0;
+#pragma unroll
+    for (int w = 0; w < FEW / 64; w++) {
+        u += n_less[w];
+        count += n_all[w];
+    }
+    ln_store<NT, PER>(acc, grads_out + (size_t)u * H, H);
+    if (threadIdx.x == 0) {
+        tokens_out[u] = own;
+        if (i == 0) *count_out = count;                              // (position 0 is its token's first)
+    }
+}
+
+struct EmbedBackward {
+    const int32_t *ids;
+    const __half *grad, *E, *g;
+    int M, V, H;
+    float eps;
+    Place *places;
+    uint8_t *first;
+    float *parts;
+    int32_t *tokens_out;
+    float *grads_out;
+    int32_t *count_out;
+};
+template <int NT, int PER>
+int embed_backward(const EmbedBackward &c, hipStream_t st) {
+    if (c.M <= FEW && (size_t)c.M * c.H <= FEW_VALUES) {
+        k_embed_backward_few<NT, PER><<<c.M, NT, 0, st>>>(c.ids, c.grad, c.M, c.V, c.H, c.E, c.g, c.eps, c.tokens_out, c.grads_out, c.count_out);
+        HIP_TRY(hipGetLastError());
+        return PETALS_OK;
+    }
+    const int runs = c.M < RUN_PIECE ? 0 : (c.M + RUN_PIECE - 1) / RUN_PIECE, pieces = runs * ((c.H + PIECE_COLUMNS - 1) / PIECE_COLUMNS);
+    k_token_places<<<(c.M + PLACE_ROWS - 1) / PLACE_ROWS, 1024, 0, st>>>(c.ids, c.M, c.V, c.places, c.first);
+    HIP_TRY(hipGetLastError());
+    k_embed_backward<NT, PER><<<pieces + c.M, NT, 0, st>>>(c.grad, c.M, c.H, c.E, c.g, c.eps, c.places, c.first, pieces, c.parts, c.tokens_out,
+                                                           c.grads_out, c.count_out);
+    HIP_TRY(hipGetLastError());
+    if (runs) {
+        k_embed_backward_join<NT, PER><<<runs, NT, 0, st>>>(c.M, c.H, c.E, c.g, c.eps, c.places, c.first, c.parts, c.tokens_out, c.grads_out);
+        HIP_TRY(hipGetLastError());
+    }
+    return PETALS_OK;
 }
 
 int check_call(const petals_client_config &cfg, int32_t M) {
@@ -797,21 +884,16 @@ int petals_client_embed_backward(petals_client *client, const int32_t *token_ids
     if (int rc = check_call(*c.cfg, M)) return rc;
     if (M > PETALS_BACKWARD_ROWS_MAX) return ps_fail(PETALS_ERR_UNSUPPORTED, "%d rows exceed %d", M, PETALS_BACKWARD_ROWS_MAX);
     if (token_ids == tokens_out) return ps_fail(PETALS_ERR_INVALID_ARG, "token_ids and tokens_out alias");
-    const int V = c.cfg->vocab, H = c.cfg->hidden;
+    const int H = c.cfg->hidden;
     // M places of 16 bytes and their flags, then a row of partial sums for every RUN_PIECE places: some 17 M + (M / 32 + 1) 4 H bytes
     Place *places = (Place *)c.scratch;
     uint8_t *first = (uint8_t *)(places + M);
     float *parts = (float *)(c.scratch + ((size_t)(first - c.scratch) + M + 255) / 256 * 256);
+    const EmbedBackward call{token_ids, (const __half *)grad_hidden, (const __half *)c.p->embeddings, (const __half *)c.p->emb_ln_g, M, c.cfg->vocab, H,
+                             c.cfg->ln_eps, places, first, parts, tokens_out, grads_out, count_out};
     hipStream_t st = (hipStream_t)stream;
-    const __half *E = (const __half *)c.p->embeddings, *g = (const __half *)c.p->emb_ln_g, *gr = (const __half *)grad_hidden;
-    const float eps = c.cfg->ln_eps;
-    k_token_places<<<(M + PLACE_ROWS - 1) / PLACE_ROWS, 1024, 0, st>>>(token_ids, M, V, places, first);
-    if (H <= 2048) embed_backward<256, 1>(gr, M, H, E, g, eps, places, first, parts, tokens_out, grads_out, count_out, st);
-    else if (H <= 4096) embed_backward<512, 1>(gr, M, H, E, g, eps, places, first, parts, tokens_out, grads_out, count_out, st);
-    else if (H <= 8192) embed_backward<1024, 1>(gr, M, H, E, g, eps, places, first, parts, tokens_out, grads_out, count_out, st);
-    else embed_backward<1024, 2>(gr, M, H, E, g, eps, places, first, parts, tokens_out, grads_out, count_out, st);
-    HIP_TRY(hipGetLastError());
-    return PETALS_OK;
+    return H <= 2048 ? embed_backward<256, 1>(call, st) : H <= 4096 ? embed_backward<512, 1>(call, st)
+                     : H <= 8192 ? embed_backward<1024, 1>(call, st) : embed_backward<1024, 2>(call, st);
 }
 
 }  // extern "C"

@@ -499,3 +499,46 @@ def test_the_most_rows_of_the_backward_calls():
     tol = _norm_error(2 * U32 * mass, E[rtok], vec[0]) + U32 * np.abs(ref) + 1e-12 * np.abs(ref).max()
     assert (np.abs(grads[:n] - ref) <= tol).all()
     c.close()
+
+
+# the border of the calls that go in one launch (128 positions, 2^19 values), a position's first and last appearance across waves
+@pytest.mark.parametrize("H,M", [(64, 127), (64, 128), (64, 129), (1088, 128), (2048, 100), (2112, 128), (4096, 128), (4160, 126), (8192, 64), (8256, 63),
+                                 (16384, 32), (16384, 33), (14336, 36), (14336, 37)])
+@pytest.mark.parametrize("kind", ["one", "turn", "reverse", "pairs", "outside"])
+def test_embed_backward_around_the_smallest_calls(H, M, kind):
+    V = 300
+    c, E, vec = _client(V, H, M, seed=25)
+    r = np.random.default_rng([26, H, M])
+    ids = {"one": np.full(M, 7), "turn": np.arange(M) % 16, "reverse": np.arange(M)[::-1], "pairs": np.arange(M) // 2 * 3 % 64,
+           "outside": r.integers(-3, 3, M) * 200}[kind].astype(np.int32)
+    dy = r.standard_normal((M, H)).astype(np.float16)
+    out = (torch.full((M,), -7, dtype=torch.int32, device=DEV), torch.full((M, H), 77.0, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV))
+    tokens, grads, count = [to_np(a) for a in c.embed_backward(to_dev(ids), to_dev(dy), out=out)]
+    rtok, ref = of.embed_backward(ids, dy, E, vec[0])
+    n = len(rtok)
+    assert count[0] == n and np.array_equal(tokens[:n], rtok)
+    assert (tokens[n:] == -7).all() and (grads[n:] == 77.0).all()
+    place = np.searchsorted(rtok, np.clip(ids, 0, V - 1))
+    mass = np.zeros((n, H))
+    np.add.at(mass, place, np.abs(dy.astype(np.float64)))
+    tol = _norm_error((np.bincount(place).max() + 1) * U32 * mass, E[rtok], vec[0]) + U32 * np.abs(ref) + 1e-12 * np.abs(ref).max()
+    assert (np.abs(grads[:n] - ref) <= tol).all()
+    c.close()
+
+
+# lists of up to 64 keys: rising logits (every key enters), falling ones, many equal, infinities below, at every size of a join
+@pytest.mark.parametrize("V,M", [(64, 3), (100, 2), (4096, 2), (4097, 2), (20000, 3), (70000, 1100), (250880, 2)])
+@pytest.mark.parametrize("K", [1, 2, 17, 63, 64])
+def test_the_best_of_rows_in_any_order(V, M, K):
+    c, _, _ = _client(V, 64, M, seed=27)
+    r = np.random.default_rng([28, V, M])
+    x = r.standard_normal((M, V)).astype(np.float32)
+    x[0] = np.arange(V, dtype=np.float32) / V                     # the best come last
+    x[1] = -np.arange(V, dtype=np.float32) / V
+    if M > 2:
+        x[2] = r.integers(0, 3, V)
+    x[-1, r.permutation(V)[:V - V // 3 - 30]] = -np.inf
+    some = [0, 1, min(2, M - 1), M // 2, M - 1]
+    top = to_np(c.logprobs(to_dev(x), None, 1.0, K)[2])[some]
+    assert np.array_equal(top, np.argsort(-x[some].astype(np.float64), axis=1, kind="stable")[:, :K])
+    c.close()
