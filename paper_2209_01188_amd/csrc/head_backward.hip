@@ -271,12 +271,14 @@ HeadPlan head_plan(const petals_client_config &cfg, int M) {
     p.pair = M <= PETALS_HEAD_BACKWARD_PAIR_ROWS;
     p.sections = (p.kt + head_section_kt(p.pair) - 1) / head_section_kt(p.pair);
     p.nb_n = (cfg.hidden + 255) / 256;
-    // Tokens of a block and splits of the contraction: the fewest stages one after the other, each at what it was measured to
-    // take (ns; 351 rows x 50257 x 2560 and 768 x 100003 x 4096), and the partial sums written and read.
-    const int shapes[3][2] = {{128, 520}, {192, 750}, {256, 860}}, one[1][2] = {{M <= 32 ? 32 : 64, 500}};
+    // Tokens of a block and splits of the contraction: the fewest stages one after the other, each at what it takes (ns; measured at 351
+    // rows x 50257 x 2560 and 768 x 100003 x 4096), and the partial sums' way to memory and back, 8 bytes of each at 2.4 TB/s.  (With 520
+    // for 128 tokens and 9.6 TB/s, without 160: 300 rows x 50257 x 4096 190 us instead of 175, 1024 x 60000 x 14336 1763 instead of 1650,
+    // 512 x 50257 x 1024 113 instead of 101.  Blocks of 224 tokens spill: 400 x 50257 x 4096 193 instead of 181.)
+    const int shapes[4][2] = {{128, 560}, {160, 650}, {192, 750}, {256, 860}}, one[1][2] = {{M <= 32 ? 32 : 64, 500}};
     const int(*shape)[2] = p.pair ? one : shapes;
     double best = 0.0;
-    for (int i = 0; i < (p.pair ? 1 : 3); i++) {
+    for (int i = 0; i < (p.pair ? 1 : 4); i++) {
         const int nb_m = (M + shape[i][0] - 1) / shape[i][0], blocks = nb_m * p.nb_n;
         int before = 0;
         for (int rounds = 1; rounds <= 8; rounds++) {
@@ -284,7 +286,7 @@ HeadPlan head_plan(const petals_client_config &cfg, int M) {
             if (want <= before) continue;
             before = want;
             const int kt_per = (p.kt / 4 + want - 1) / want * 4, splits = (p.kt + kt_per - 1) / kt_per;
-            const double ns = (double)(((long long)blocks * splits + UNITS - 1) / UNITS) * kt_per * shape[i][1] + splits * (double)M * cfg.hidden / 1200.0;
+            const double ns = (double)(((long long)blocks * splits + UNITS - 1) / UNITS) * kt_per * shape[i][1] + splits * (double)M * cfg.hidden / 300.0;
             if (best == 0.0 || ns < best) {
                 best = ns;
                 p.bm = shape[i][0];
@@ -295,7 +297,7 @@ HeadPlan head_plan(const petals_client_config &cfg, int M) {
             if (p.pair) break;
         }
         if (!before) {                // more blocks than eight rounds hold
-            const double ns = (double)((blocks + UNITS - 1) / UNITS) * p.kt * shape[i][1] + (double)M * cfg.hidden / 1200.0;
+            const double ns = (double)((blocks + UNITS - 1) / UNITS) * p.kt * shape[i][1] + (double)M * cfg.hidden / 300.0;
             if (best == 0.0 || ns < best) {
                 best = ns;
                 p.bm = shape[i][0];
@@ -390,6 +392,7 @@ int petals_client_lm_head_backward(petals_client *client, void *dev_store, const
     e = p.bm == 32    ? head_block<32, true>(p, E, store, M, V, H, st)
         : p.bm == 64  ? head_block<64, true>(p, E, store, M, V, H, st)
         : p.bm == 128 ? head_block<128, false>(p, E, store, M, V, H, st)
+        : p.bm == 160 ? head_block<160, false>(p, E, store, M, V, H, st)
         : p.bm == 192 ? head_block<192, false>(p, E, store, M, V, H, st)
                       : head_block<256, false>(p, E, store, M, V, H, st);
     HIP_TRY(e);

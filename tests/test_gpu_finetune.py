@@ -542,3 +542,14 @@ def test_the_best_of_rows_in_any_order(V, M, K):
     top = to_np(c.logprobs(to_dev(x), None, 1.0, K)[2])[some]
     assert np.array_equal(top, np.argsort(-x[some].astype(np.float64), axis=1, kind="stable")[:, :K])
     c.close()
+
+
+# the block sizes 128, 160, 192 and 256, each full, one row short and one row into the next block
+@pytest.mark.parametrize("M", [127, 129, 159, 160, 161, 191, 193, 255, 256, 320, 321, 385])
+def test_lm_head_backward_at_the_blocks_of_tokens(M):
+    V, H = 6007, 2112
+    c, E, vec = _client(V, H, M, seed=29)
+    r = np.random.default_rng([30, M])
+    x = r.standard_normal((M, H)).astype(np.float16)
+    _check_head(c, E, vec[2], x, _softmax_grad(r, M, V))
+    c.close()
