@@ -544,10 +544,10 @@ def test_the_best_of_rows_in_any_order(V, M, K):
     c.close()
 
 
-# the block sizes 128, 160, 192 and 256, each full, one row short and one row into the next block
-@pytest.mark.parametrize("M", [127, 129, 159, 160, 161, 191, 193, 255, 256, 320, 321, 385])
-def test_lm_head_backward_at_the_blocks_of_tokens(M):
-    V, H = 6007, 2112
+# blocks of 128, 160, 192 and 256 tokens, with one or several to a call, full and ragged
+@pytest.mark.parametrize("V,H,M", [(6007, 2112, 127), (6007, 2112, 129), (6007, 2112, 385), (30011, 2560, 129), (30011, 2560, 160), (20011, 4096, 257),
+                                   (8009, 14336, 161), (8009, 14336, 192), (777, 8192, 2000), (777, 16384, 1000), (777, 16384, 1024)])
+def test_lm_head_backward_at_the_blocks_of_tokens(V, H, M):
     c, E, vec = _client(V, H, M, seed=29)
     r = np.random.default_rng([30, M])
     x = r.standard_normal((M, H)).astype(np.float16)
