@@ -269,31 +269,34 @@ template <int JOIN_NT>
 __global__ void __launch_bounds__(JOIN_NT) k_logprobs_join(LogprobsOut o, int V, int splits, double invT, int top_k,
                                                            const RowStat *__restrict__ stats, const uint64_t *__restrict__ tops) {
     constexpr int JOIN_NW = JOIN_NT / 64;
-    __shared__ RowStat sm[JOIN_NW];
     __shared__ uint64_t lists[JOIN_NW][2 * LIST], firsts[LOGPROBS_GROUPS + 2 * LIST], bound;
-    const int t = blockIdx.x, n = splits * top_k;
+    const int t = blockIdx.x, n = splits * top_k, lane = threadIdx.x & 63;
+    const uint64_t *keys = tops + (size_t)t * n;
+    uint64_t key = (int)threadIdx.x < n ? keys[threadIdx.x] : 0;                   // (asked for early)
     RowStat s{-INFINITY, 0.0, 0.0};
-    for (int i = threadIdx.x; i < splits; i += JOIN_NT) merge(s, stats[(size_t)t * splits + i], invT);
+    for (int i = lane; i < splits; i += 64) merge(s, stats[(size_t)t * splits + i], invT);          // by every wave
     if (top_k) {
-        const uint64_t *keys = tops + (size_t)t * n;
         const int each = min(top_k, (2 * top_k + splits - 1) / splits), some = splits * each;          // top_k .. splits + 2 top_k
         for (int i = threadIdx.x; i < some; i += JOIN_NT) firsts[i] = keys[i / each * top_k + i % each];
         if (threadIdx.x == 0) bound = 0;
         __syncthreads();
         for (int i = threadIdx.x; i < some; i += JOIN_NT) {
-            const uint64_t key = firsts[i];
+            const uint64_t f = firsts[i];
             int larger = 0;
 #pragma unroll 8
-            for (int j = 0; j < some; j++) larger += firsts[j] > key;
-            if (key && larger == top_k - 1) bound = key - 1;
+            for (int j = 0; j < some; j++) larger += firsts[j] > f;
+            if (f && larger == top_k - 1) bound = f - 1;
         }
         __syncthreads();
         TopList list(lists);
         list.floor = bound;
-        for (int i = threadIdx.x; i < (n + 63) / 64 * 64; i += JOIN_NT) list.offer(i < n ? keys[i] : 0, top_k);
+        for (int i = threadIdx.x; i < (n + 63) / 64 * 64; i += JOIN_NT) {
+            list.offer(key, top_k);
+            key = i + JOIN_NT < n ? keys[i + JOIN_NT] : 0;
+        }
         list.join(lists, top_k, min(JOIN_NW, (n + 63) / 64));
     }
-    s = block_merge<JOIN_NW>(s, invT, sm);
+    s = wave_merge(s, invT);
     logprobs_store(o, t, V, invT, top_k, s, lists[0]);
 }
 
