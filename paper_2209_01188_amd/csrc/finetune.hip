@@ -150,19 +150,20 @@ __device__ __forceinline__ int larger_in(const uint64_t *list, uint64_t key) {
     for (int step = LIST / 2; step; step /= 2) n += list[n + step - 1] > key ? step : 0;
     return n + (list[n] > key);
 }
+// the rank-th largest of a wave's values (at least that many are as large)
+__device__ __forceinline__ float wave_ranked(float v, int rank) {
+    int above = 0;
+#pragma unroll
+    for (int i = 0; i < 64; i++) above += __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), i)) > v;
+    return -wave_max(above < rank ? -v : -INFINITY);
+}
 struct TopList {
     uint64_t *list;                                // of this wave, in LDS: its list, and what waits
     uint64_t floor = 0;                            // what is no larger does not come in
     int waiting = 0;
     __device__ __forceinline__ TopList(uint64_t (*lists)[2 * LIST]) : list(lists[threadIdx.x >> 6]) { list[threadIdx.x & 63] = 0; }
-    // most: every lane's largest logit of its first step.  The top_k-th largest of the 64 lanes' is a bound that at least top_k
-    // logits of the step reach.
-    __device__ __forceinline__ void start(float most, int top_k) {
-        int above = 0;
-#pragma unroll
-        for (int i = 0; i < 64; i++) above += __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(most), i)) > most;
-        floor = ((uint64_t)order_key(-wave_max(above < top_k ? -most : -INFINITY)) << 32) - 1;
-    }
+    // from here on only values from this one on
+    __device__ __forceinline__ void start(float value) { floor = ((uint64_t)order_key(value) << 32) - 1; }
     __device__ __forceinline__ void offer(uint64_t key, int top_k) {      // one key per lane, 0: none
         unsigned long long who = __ballot(key > floor);
         if (!who) return;
@@ -236,13 +237,26 @@ __global__ void __launch_bounds__(ROW_NT) k_logprobs(LogprobsOut o, int V, int r
                                                      uint64_t *__restrict__ tops) {
     __shared__ RowStat sm[ROW_NW];
     __shared__ uint64_t lists[ROW_NW][2 * LIST];
+    __shared__ float sf[ROW_NW];
     const int t = blockIdx.y, lane = threadIdx.x & 63, begin = blockIdx.x * range, end = min(V, begin + range);
+    const bool all_waves = begin + (ROW_NW - 1) * WAVE_STEP < end;
     const float c = (float)(invT * LOG2E);
     RowStat s{-INFINITY, 0.0, 0.0};
     TopList list(lists);
     walk_row<ROW_NT>(o.logits + (size_t)t * V, begin, end, [&](int v0, const float (&l)[ROW_PER]) {
         const float most = accumulate<ROW_PER, true>(s, l, c, invT);
-        if (top_k && v0 < begin + ROW_STEP) list.start(most, top_k);
+        // The bound to begin with: of each lane's largest of the first step, at least top_k in the workgroup are as large, if all waves have
+        // some; else in the wave.
+        if (top_k && v0 < begin + ROW_STEP) {
+            float bound = wave_ranked(most, all_waves ? (top_k + ROW_NW - 1) / ROW_NW : top_k);
+            if (all_waves) {
+                if (lane == 0) sf[threadIdx.x >> 6] = bound;
+                __syncthreads();
+#pragma unroll
+                for (int w = 0; w < ROW_NW; w++) bound = fminf(bound, sf[w]);
+            }
+            list.start(bound);
+        }
         if (top_k && __ballot(!(most < key_value(list.floor + 1)))) {
 #pragma unroll
             for (int i = 0; i < ROW_PER; i++) {
