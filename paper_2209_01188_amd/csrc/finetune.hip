@@ -128,9 +128,10 @@ __device__ __forceinline__ void walk_row(const float *row, int begin, int end, F
 //
 // A key is (value, lower index first) as one 64-bit number; no two are equal.  A wave keeps the best keys it has seen in falling order
 // in LDS.  A step's logits are compared with the last key that still counts; what passes, after the first few hundred logits of random
-// order little, waits in LDS as well, and goes in many at a time: each key's place in the list is the number of larger ones.  (Inserted
-// one by one, 120 cycles each: the 50 best of 1 x 250880 54 us instead of 20, of 300 x 50257 87 instead of 45, of 2048 x 250880 456
-// instead of 405; of the 5 best of 1 x 250880 11.5 instead of 13.)
+// order little, waits in LDS as well, and goes in many at a time: each key's place in the list is the number of larger ones.  The waves
+// of a workgroup share what they know of the top_k-th best.  (Keys inserted one by one, 120 cycles each, every wave for itself: the 50
+// best of 1 x 250880 54 us instead of 18, of 300 x 50257 87 instead of 38, of 2048 x 250880 456 instead of 376; the 5 best of 1 x 250880
+// 11.5 instead of 13.)
 __device__ __forceinline__ uint32_t order_key(float f) {                   // orders like the floats (-0 as +0)
     const uint32_t u = __float_as_uint(f + 0.0f);
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
@@ -159,6 +160,9 @@ __device__ __forceinline__ float wave_ranked(float v, int rank) {
 }
 struct TopList {
     uint64_t *list;                                // of this wave, in LDS: its list, and what waits
+    // What every wave has a share of the top_k keys of, in LDS: all together have top_k that reach the lowest of these.  (They rise while
+    // others read them; an old one is a bound as well, so the results do not depend on when it is read.)
+    volatile uint64_t *reached = nullptr;
     uint64_t floor = 0;                            // what is no larger does not come in
     int waiting = 0;
     __device__ __forceinline__ TopList(uint64_t (*lists)[2 * LIST]) : list(lists[threadIdx.x >> 6]) { list[threadIdx.x & 63] = 0; }
@@ -187,7 +191,15 @@ struct TopList {
         place(a, at_a, b, at_b);
         waiting = 0;
         floor = max(floor, list[top_k - 1]);
+        if (reached) {
+            if (lane == 0) reached[threadIdx.x >> 6] = list[share(top_k) - 1];
+            uint64_t lowest = reached[0];
+#pragma unroll
+            for (int w = 1; w < ROW_NW; w++) lowest = min(lowest, (uint64_t)reached[w]);
+            floor = max(floor, lowest);
+        }
     }
+    static __device__ __forceinline__ int share(int top_k) { return (top_k + ROW_NW - 1) / ROW_NW; }
     // the list becomes these keys at their places (of those that are none, 0, there may be several at one place)
     __device__ __forceinline__ void place(uint64_t a, int at_a, uint64_t b, int at_b) {
         list[threadIdx.x & 63] = 0;
@@ -237,6 +249,7 @@ __global__ void __launch_bounds__(ROW_NT) k_logprobs(LogprobsOut o, int V, int r
                                                      uint64_t *__restrict__ tops) {
     __shared__ RowStat sm[ROW_NW];
     __shared__ uint64_t lists[ROW_NW][2 * LIST];
+    __shared__ uint64_t reached[ROW_NW];
     __shared__ float sf[ROW_NW];
     const int t = blockIdx.y, lane = threadIdx.x & 63, begin = blockIdx.x * range, end = min(V, begin + range);
     const bool all_waves = begin + (ROW_NW - 1) * WAVE_STEP < end;
@@ -248,10 +261,14 @@ __global__ void __launch_bounds__(ROW_NT) k_logprobs(LogprobsOut o, int V, int r
         // The bound to begin with: of each lane's largest of the first step, at least top_k in the workgroup are as large, if all waves have
         // some; else in the wave.
         if (top_k && v0 < begin + ROW_STEP) {
-            float bound = wave_ranked(most, all_waves ? (top_k + ROW_NW - 1) / ROW_NW : top_k);
+            float bound = wave_ranked(most, all_waves ? TopList::share(top_k) : top_k);
             if (all_waves) {
-                if (lane == 0) sf[threadIdx.x >> 6] = bound;
+                if (lane == 0) {
+                    sf[threadIdx.x >> 6] = bound;
+                    reached[threadIdx.x >> 6] = 0;
+                }
                 __syncthreads();
+                list.reached = reached;
 #pragma unroll
                 for (int w = 0; w < ROW_NW; w++) bound = fminf(bound, sf[w]);
             }
