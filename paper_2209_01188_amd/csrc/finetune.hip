@@ -18,7 +18,7 @@ namespace {
 // well); the sums are fp64, so that S - 1, what is left beside the largest token, keeps its digits where that token has
 // nearly everything: log S and -D / S are the two parts of the entropy, both >= 0, and nothing cancels between them.
 //
-// Bound by the bytes of the logits where there are many rows: 1024 x 250880 with the 20 best of each in 194 us, 5.3 TB/s (a copy
+// Bound by the bytes of the logits where there are many rows: 1024 x 250880 with the 20 best of each in 189 us, 5.4 TB/s (a copy
 // within the memory reaches 4.8); with few rows by the latency of two launches, 1 x 250880 in 13 us with 5 of them, in 20 with 50.
 constexpr double LN2 = 0.69314718055994530942, LOG2E = 1.4426950408889634074;
 
@@ -337,7 +337,7 @@ __global__ void __launch_bounds__(JOIN_NT) k_logprobs_join(LogprobsOut o, int V,
 // second finds the logits in the cache in front of the memory, and workgroups that read run beside others that write.  Fewer rows are cut
 // into parts, with a launch for each pass.
 //
-// Bound by the memory: 2048 x 250880 in 871 us (a copy of the logits takes 862), 701 x 50257 in 74 (59).  Rows as a whole against parts with
+// Bound by the memory: 2048 x 250880 in 875 us (a copy of the logits takes 862), 701 x 50257 in 74 (59).  Rows as a whole against parts with
 // a launch for each pass: 64 x 250880 54 and 37 us, 128 67 and 68, 191 94 and 100; 2048 x 50257 196 and 303, 300 x 50257 39 and 44.
 // 512 against 1024 threads to a row: 300 x 20000 20 and 25 us, 701 x 50257 71 and 72, 701 x 100003 140 and 133, 2048 x 250880 1086 and 955.
 struct DistillIn {
