@@ -14,9 +14,9 @@
  * Every call can be captured into a graph.  The same inputs give the same bits in every call.
  *
  * Logits may be -infinity (a token that is ruled out: probability 0).  A row of which no logit is
- * above -infinity has no distribution; each call says what it returns for one.  A row with a NaN or
- * +infinity gives NaN for that row's real-valued results (and in-range token ids); other rows are
- * not affected.
+ * above -infinity has no distribution; each call says what it returns for one.  A row of logits with
+ * a NaN or +infinity gives NaN for that row's real-valued results (and in-range token ids); other rows
+ * are not affected.  Outputs may overlap neither inputs nor each other, but for what is said below.
  */
 #ifndef PETALS_FINETUNE_H
 #define PETALS_FINETUNE_H
@@ -61,6 +61,7 @@ int petals_client_logprobs(petals_client *client, const float *logits, const int
  *   loss_grad         dev fp32 [M], NULL: 1
  *   loss_out          dev fp32 [M], may be NULL if grad_logits_out is given
  *   grad_logits_out   dev fp32 [M, V], may be NULL if loss_out is given; may be the same memory as logits
+ * A NaN or +infinity among a row's teacher_logits makes its loss and the gradients of the listed tokens NaN.
  * A row without a list (no entry, or all teacher logits -infinity) has loss 0 and gradient 0.  A row without a distribution
  * of its own (and with a list) has loss +infinity and gradient 0.  1 <= K <= PETALS_DISTILL_TOP_MAX, above it
  * PETALS_ERR_UNSUPPORTED; temperature at least 1e-38 and not infinite; M <= max_rows_per_call, else PETALS_ERR_CAPACITY.
@@ -74,7 +75,7 @@ int petals_client_distill(petals_client *client, const float *logits, int32_t M,
  *   grad_hidden_out[t] = J_t (sum_v grad_logits[t][v] * embeddings[v]),  J_t the derivative of the final LayerNorm at hidden_in[t]
  *   hidden_in         dev fp16 [M, H]: what petals_client_lm_head was given
  *   grad_logits       dev fp32 [M, V], finite
- *   grad_hidden_out   dev fp16 [M, H]: grad_out of petals_span_backward; may not overlap the inputs
+ *   grad_hidden_out   dev fp16 [M, H]: grad_out of petals_span_backward
  * (The roundings of the forward pass count as the identity; matrix and LayerNorm parameters are frozen.)  The product runs on
  * fp16 matrix instructions with fp32 sums; grad_logits is taken as two fp16 values for calls of up to
  * PETALS_HEAD_BACKWARD_PAIR_ROWS rows and as one beyond, scaled per row and section of the vocabulary (1024 columns, beyond
@@ -82,7 +83,8 @@ int petals_client_distill(petals_client *client, const float *logits, int32_t M,
  * the largest, two by 2^-22 down to 2^-18.  grad_hidden_out is rounded to
  * fp16 once, without loss scaling (loss_grad of petals_client_distill can carry a scale).
  * dev_store: 256-byte aligned device memory of petals_client_lm_head_backward_bytes(cfg, M) bytes, contents unspecified
- * before and after.  M <= max_rows_per_call, else PETALS_ERR_CAPACITY.
+ * before and after.  (That many for a call of M rows: one of fewer rows may need more, being cut up in another way, so a store that
+ * serves calls of several sizes has the most that any of them asks for.)  M <= max_rows_per_call, else PETALS_ERR_CAPACITY.
  */
 #define PETALS_HEAD_BACKWARD_PAIR_ROWS 64
 int petals_client_lm_head_backward_bytes(const petals_client_config *cfg, int32_t M, size_t *bytes);
@@ -98,7 +100,7 @@ int petals_client_lm_head_backward(petals_client *client, void *dev_store, const
  *   grads_out         dev fp32 [M, H]: row i = the gradient of embeddings[tokens_out[i]], through the LayerNorm behind the lookup
  *   count_out         dev int32 [1]: how many there are; entries of the two outputs from there on are left as they were
  * The rows of a token are summed in fp32 in an order that depends on H and on their number alone, then go through the
- * derivative of the LayerNorm once.  Outputs may not overlap the inputs.  M <= max_rows_per_call, else PETALS_ERR_CAPACITY.
+ * derivative of the LayerNorm once.  M <= max_rows_per_call, else PETALS_ERR_CAPACITY.
  */
 int petals_client_embed_backward(petals_client *client, const int32_t *token_ids, const void *grad_hidden, int32_t M,
                                  int32_t *tokens_out, float *grads_out, int32_t *count_out, void *stream);

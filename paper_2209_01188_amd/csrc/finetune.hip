@@ -886,6 +886,11 @@ int petals_client_distill(petals_client *client, const float *logits, int32_t M,
     if (K < 1) return ps_fail(PETALS_ERR_INVALID_ARG, "K must be positive");
     if (K > PETALS_DISTILL_TOP_MAX) return ps_fail(PETALS_ERR_UNSUPPORTED, "K %d exceeds %d", K, PETALS_DISTILL_TOP_MAX);
     if (!loss_out && !grad_logits_out) return ps_fail(PETALS_ERR_INVALID_ARG, "neither loss nor gradient requested");
+    const void *const outs[] = {loss_out, grad_logits_out}, *const ins[] = {teacher_tokens, teacher_logits, loss_grad};
+    for (const void *o : outs)
+        for (const void *i : ins)
+            if (o && o == i) return ps_fail(PETALS_ERR_INVALID_ARG, "an output and an input alias");
+    if (loss_out == logits || loss_out == grad_logits_out) return ps_fail(PETALS_ERR_INVALID_ARG, "loss and logits or gradient alias");
     if (!usable_temperature(temperature)) return ps_fail(PETALS_ERR_INVALID_ARG, "temperature must be positive and finite");
     hipStream_t st = (hipStream_t)stream;
     const int V = c.cfg->vocab;
@@ -917,7 +922,7 @@ int petals_client_embed_backward(petals_client *client, const int32_t *token_ids
     const ps_client_view c = ps_view(client);
     if (int rc = check_call(*c.cfg, M)) return rc;
     if (M > PETALS_BACKWARD_ROWS_MAX) return ps_fail(PETALS_ERR_UNSUPPORTED, "%d rows exceed %d", M, PETALS_BACKWARD_ROWS_MAX);
-    if (token_ids == tokens_out) return ps_fail(PETALS_ERR_INVALID_ARG, "token_ids and tokens_out alias");
+    if (token_ids == tokens_out || grad_hidden == (const void *)grads_out) return ps_fail(PETALS_ERR_INVALID_ARG, "an output and an input alias");
     const int H = c.cfg->hidden;
     // M places of 16 bytes and their flags, then a row of partial sums for every RUN_PIECE places: some 17 M + (M / 32 + 1) 4 H bytes
     Place *places = (Place *)c.scratch;

@@ -73,6 +73,18 @@ def test_distill_refusals(client):
         assert call(T=T) == INVALID
 
 
+def test_distill_refuses_outputs_over_inputs(client):
+    L, f = b.lib(), C.c_float
+    logits, ids, vals, w, loss, grad = FAKE[:6]
+    for bad_loss, bad_grad in ((loss, vals), (loss, w), (loss, ids), (w, grad), (vals, grad), (ids, None), (logits, grad), (grad, grad)):
+        assert L.petals_client_distill(client, logits, 4, ids, vals, 3, f(1.0), w, bad_loss, bad_grad, None) == INVALID
+
+
+def test_embed_backward_refuses_outputs_over_inputs(client):
+    ids, dy, tok, n = FAKE[:4]
+    assert b.lib().petals_client_embed_backward(client, ids, dy, 4, tok, dy, n, None) == INVALID
+
+
 def test_lm_head_backward_refusals(client):
     L = b.lib()
     store, x, g, out = FAKE[:4]

@@ -553,3 +553,91 @@ def test_lm_head_backward_at_the_blocks_of_tokens(V, H, M):
     x = r.standard_normal((M, H)).astype(np.float16)
     _check_head(c, E, vec[2], x, _softmax_grad(r, M, V))
     c.close()
+
+
+# rows that one workgroup takes as a whole: the number of rows from which on it does, both widths of workgroup, vocabularies beside them
+@pytest.mark.parametrize("V,M,K,T", [(1, 192, 1, 1.0), (7, 200, 7, 2.0), (100, 191, 100, 1.0), (1000, 193, 130, 0.5), (8193, 256, 1024, 1.0),
+                                     (65536, 192, 64, 2.0), (65537, 192, 64, 2.0), (100003, 194, 1, 1.0)])
+def test_distillation_by_whole_rows(V, M, K, T):
+    c, _, _ = _client(V, 64, M)
+    r, x = _logits(M, V, 31)
+    ids = r.integers(-1, V, (M, K)).astype(np.int32)
+    vals = (r.standard_normal((M, K)) * 3).astype(np.float32)
+    ids[1], vals[2], x[3] = -1, -np.inf, -np.inf           # no list, a list of nothing, no distribution
+    if V > 1:
+        ids[3, 0] = 0
+        x[4, V // 2:] = -np.inf
+        ids[4] = 0
+    w = (r.random(M) + 0.5).astype(np.float32)
+    loss, grad = _check_distill(c, x, ids, vals, T, w)
+    loss2, grad2 = _check_distill(c, x, ids, vals, T, w, dev=_shifted(x), in_place=True)
+    assert np.array_equal(loss, loss2) and np.array_equal(grad, grad2)
+    only, none = c.distill(to_dev(x), to_dev(ids), to_dev(vals), T, w if w is None else to_dev(w), want_grad=False)
+    assert none is None and np.array_equal(to_np(only), loss)
+    c.close()
+
+
+@pytest.mark.parametrize("M", [3, 40, 150, 300, 1000])
+def test_a_first_call_inside_a_capture(M):
+    """No call before it that could have prepared something; eager work between the replays."""
+    V, H = 2003, 4160
+    c, E, vec = _client(V, H, M, seed=32)
+    r, x = _logits(M, V, 33)
+    logits, hid = to_dev(x), to_dev(r.standard_normal((M, H)).astype(np.float16))
+    ids, vals = to_dev(r.integers(0, V, (M, 4)).astype(np.int32)), to_dev(r.standard_normal((M, 4)).astype(np.float32))
+    tokens = to_dev(r.integers(0, V, M).astype(np.int32))
+    store = torch.empty(binding.petals_client_lm_head_backward_bytes(c.cfg, M), dtype=torch.uint8, device=DEV)
+
+    def step():
+        out = list(c.logprobs(logits, tokens, 1.0, 50)) + list(c.distill(logits, ids, vals, 2.0))
+        out.append(c.lm_head_backward(hid, out[-1], store=store))
+        return out + list(c.embed_backward(tokens, out[-1]))
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        captured = step()
+    for i in range(3):
+        for a in captured:
+            a.fill_(0)
+        g.replay()
+        torch.cuda.synchronize()
+        eager = step()
+        n = int(eager[-1][0])
+        for k, (a, b) in enumerate(zip(captured, eager)):
+            a, b = (a[:n], b[:n]) if k in (7, 8) else (a, b)
+            assert torch.equal(a, b), (i, k)
+        logits.mul_(0.9)
+        tokens.copy_(tokens.flip(0))
+    c.close()
+
+
+def test_two_clients_on_two_streams_at_once():
+    V, H, M = 20011, 1024, 150
+    calls = []
+    for seed in (34, 35):
+        c, E, vec = _client(V, H, M, seed=seed)
+        r, x = _logits(M, V, seed)
+        state = (to_dev(x), to_dev(r.integers(0, V, M).astype(np.int32)), to_dev(r.standard_normal((M, 1)).astype(np.float32)),
+                 to_dev(r.standard_normal((M, H)).astype(np.float16)), to_dev(r.integers(0, 90, M).astype(np.int32)))
+
+        def step(c=c, s=state):
+            lp = c.logprobs(s[0], s[1], 1.0, 20)
+            loss, dl = c.distill(s[0], s[1][:, None], s[2])
+            dx = c.lm_head_backward(s[3], dl)
+            return [*lp, loss, dl, dx, *c.embed_backward(s[4], dx)]
+        calls.append((c, step, torch.cuda.Stream()))
+    alone = [step() for _, step, _ in calls]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        both = []
+        for _, step, s in calls:
+            with torch.cuda.stream(s):
+                both.append(step())
+        torch.cuda.synchronize()
+        for a, b in zip(alone, both):
+            n = int(a[-1][0])
+            for k, (u, v) in enumerate(zip(a, b)):
+                u, v = (u[:n], v[:n]) if k in (7, 8) else (u, v)
+                assert torch.equal(u, v), k
+    for c, _, _ in calls:
+        c.close()
