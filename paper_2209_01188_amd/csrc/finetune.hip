@@ -337,9 +337,10 @@ __global__ void __launch_bounds__(JOIN_NT) k_logprobs_join(LogprobsOut o, int V,
 // second finds the logits in the cache in front of the memory, and workgroups that read run beside others that write.  Fewer rows are cut
 // into parts, with a launch for each pass.
 //
-// Bound by the memory: 2048 x 250880 in 875 us (a copy of the logits takes 862), 701 x 50257 in 74 (59).  Rows as a whole against parts with
-// a launch for each pass: 64 x 250880 54 and 37 us, 128 67 and 68, 191 94 and 100; 2048 x 50257 196 and 303, 300 x 50257 39 and 44.
-// 512 against 1024 threads to a row: 300 x 20000 20 and 25 us, 701 x 50257 71 and 72, 701 x 100003 140 and 133, 2048 x 250880 1086 and 955.
+// Bound by the memory: 2048 x 250880 in 870 us (a copy of the logits takes 862), 701 x 50257 in 74 (59).  Rows as a whole against parts with
+// a launch for each pass: 64 x 250880 54 and 36 us, 128 67 and 68, 191 94 and 100; 128 x 50257 24 and 21, 150 25 and 28, 300 39 and 44,
+// 2048 196 and 303.  512 against 1024 threads to a row: 300 x 20000 20 and 25 us, 701 x 50257 71 and 72, 701 x 100003 140 and 133, 2048 x
+// 250880 1086 and 955.  Few rows wait for two launches: 1 x 20000 12.3 us (13.2 where the workgroup of a row's first part had the list).
 struct DistillIn {
     const float *logits;
     const int32_t *ids;
@@ -355,10 +356,11 @@ struct DistillPart {                   // of a row and split
 };
 struct DistillRow {                    // of a row, by the workgroup of its first split
     double max, norm;                  // of the teacher's logits, and 1 / sum of e^((logit - max) / T)
-    double term, mass;                 // sum p (log p - z / T) and sum p: with log q = z / T - lse the loss is T^2 (term + mass lse)
+    double term, mass;                 // sum p (log p - (z - ref) / T) and sum p: with log q = z / T - lse the loss is T^2 (term + mass (lse - ref / T))
+    double ref;                        // the list's largest z, so that large logits cancel exactly
     int listed;
 };
-constexpr int DISTILL_WHOLE = 192, DISTILL_WIDE = 65536;     // rows from which on one is a workgroup's; vocabulary beyond which it has 1024 threads, not 512
+constexpr int DISTILL_WHOLE = 140, DISTILL_WIDE = 65536;     // rows from which on one is a workgroup's; vocabulary beyond which it has 1024 threads, not 512
 template <int NT>
 constexpr int LIST_PER = (PETALS_DISTILL_TOP_MAX + NT - 1) / NT;
 
@@ -371,7 +373,8 @@ __device__ __forceinline__ float teacher_entry(const DistillIn &d, int t, int k,
     return id < 0 ? -INFINITY : d.vals[(size_t)t * d.K + k];
 }
 
-template <int NT>
+// PARTS: the logits of a part of the row (part), or the list (part null); otherwise both, of the whole row
+template <int NT, bool PARTS>
 __device__ __forceinline__ void distill_stats(const DistillIn &d, int t, int split, DistillPart *part, DistillRow *out, RowStat *sm, double *sd,
                                               float *sf) {
     const float *row = d.logits + (size_t)t * d.V;
@@ -389,10 +392,18 @@ __device__ __forceinline__ void distill_stats(const DistillIn &d, int t, int spl
         some |= !(val[i] == -INFINITY);
     }
     const bool listed = __syncthreads_or(some);
-    if (split == 0) {
-        DistillRow r{0.0, 0.0, 0.0, 0.0, listed};
+    if (!PARTS || !part) {
+        DistillRow r{0.0, 0.0, 0.0, 0.0, 0.0, listed};
         if (listed) {
+            float z[LIST_PER<NT>], most = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < LIST_PER<NT>; i++) {
+                z[i] = val[i] == -INFINITY ? -INFINITY : row[id[i]];
+                most = fmaxf(most, z[i]);
+            }
             mx = block_max<NT / 64>(mx, sf);
+            most = block_max<NT / 64>(most, sf);
+            const double ref = most == -INFINITY ? 0.0 : (double)most;
             double sum = 0.0, term = 0.0, mass = 0.0;
 #pragma unroll
             for (int i = 0; i < LIST_PER<NT>; i++)
@@ -404,15 +415,16 @@ __device__ __forceinline__ void distill_stats(const DistillIn &d, int t, int spl
                 if (val[i] == -INFINITY) continue;
                 const double tt = ((double)val[i] - mx) * d.invT, p = exp_f64(tt) / sum;
                 if (!(p == 0.0)) {
-                    term += p * (tt - ls - (double)row[id[i]] * d.invT);
+                    term += p * (tt - ls - ((double)z[i] - ref) * d.invT);
                     mass += p;
                 }
             }
             term = block_sum<NT / 64>(term, sd);
             mass = block_sum<NT / 64>(mass, sd);
-            r = DistillRow{(double)mx, 1.0 / sum, term, mass, 1};
+            r = DistillRow{(double)mx, 1.0 / sum, term, mass, ref, 1};
         }
         if (threadIdx.x == 0) *out = r;
+        if (PARTS) return;
     }
     if (!listed) return;                                   // nobody reads the part
     RowStat s{-INFINITY, 0.0, 0.0};
@@ -443,7 +455,7 @@ __device__ __forceinline__ void distill_grad(const DistillIn &d, int t, int spli
     }
     const bool none = s.S == 0.0, zero = !r.listed || none;
     if (split == 0 && threadIdx.x == 0 && d.loss)
-        d.loss[t] = !r.listed ? 0.0f : none ? INFINITY : (float)(d.T * d.T * (r.term + r.mass * ((double)s.m * d.invT + log(s.S))));
+        d.loss[t] = !r.listed ? 0.0f : none ? INFINITY : (float)(d.T * d.T * (r.term + r.mass * (((double)s.m - r.ref) * d.invT + log(s.S))));
     if (!d.grad) return;
     float *out = d.grad + (size_t)t * d.V;
     const double w = d.T * (d.loss_grad ? (double)d.loss_grad[t] : 1.0);
@@ -516,13 +528,13 @@ struct DistillShared {
     int id[PETALS_DISTILL_TOP_MAX];
     double p[PETALS_DISTILL_TOP_MAX];
 };
-// workgroup (split, row), one of the two passes
+// One of the two passes, a workgroup for each row and split.  In the first, M in front of them have the lists, which take longest.
 template <bool SECOND>
-__global__ void __launch_bounds__(ROW_NT) k_distill_part(DistillIn d, DistillPart *__restrict__ parts, DistillRow *__restrict__ rows) {
+__global__ void __launch_bounds__(ROW_NT) k_distill_part(DistillIn d, int M, int splits, DistillPart *__restrict__ parts, DistillRow *__restrict__ rows) {
     __shared__ DistillShared<ROW_NT> sh;
-    const int split = blockIdx.x, splits = gridDim.x, t = blockIdx.y;
+    const int b = (int)blockIdx.x - (SECOND ? 0 : M), t = __builtin_amdgcn_readfirstlane(b < 0 ? (int)blockIdx.x : b / splits), split = b < 0 ? 0 : b - t * splits;
     if (SECOND) distill_grad<ROW_NT>(d, t, split, splits, parts + (size_t)t * splits, rows + t, sh.id, sh.p);
-    else distill_stats<ROW_NT>(d, t, split, parts + (size_t)t * splits + split, rows + t, sh.sm, sh.sd, sh.sf);
+    else distill_stats<ROW_NT, true>(d, t, split, b < 0 ? nullptr : parts + b, rows + t, sh.sm, sh.sd, sh.sf);
 }
 // both passes of row first + blockIdx.x
 template <int NT>
@@ -531,7 +543,7 @@ __global__ void __launch_bounds__(NT) k_distill_row(DistillIn d, int first) {
     __shared__ DistillPart part;
     __shared__ DistillRow row;
     const int t = first + blockIdx.x;
-    distill_stats<NT>(d, t, 0, &part, &row, sh.sm, sh.sd, sh.sf);
+    distill_stats<NT, false>(d, t, 0, &part, &row, sh.sm, sh.sd, sh.sf);
     __syncthreads();
     distill_grad<NT>(d, t, 0, 1, &part, &row, sh.id, sh.p);
 }
@@ -909,9 +921,9 @@ int petals_client_distill(petals_client *client, const float *logits, int32_t M,
     const size_t room = (c.scratch_bytes - sizeof(DistillRow) * M) / ((size_t)M * sizeof(DistillPart));
     const RowSplit sp = row_split(M, V, DISTILL_GROUPS, (int)min((size_t)1 << 20, room));
     d.range = sp.range;
-    k_distill_part<false><<<dim3(sp.splits, M), ROW_NT, 0, st>>>(d, parts, rows);
+    k_distill_part<false><<<M + M * sp.splits, ROW_NT, 0, st>>>(d, M, sp.splits, parts, rows);
     HIP_TRY(hipGetLastError());
-    k_distill_part<true><<<dim3(sp.splits, M), ROW_NT, 0, st>>>(d, parts, rows);
+    k_distill_part<true><<<M * sp.splits, ROW_NT, 0, st>>>(d, M, sp.splits, parts, rows);
     HIP_TRY(hipGetLastError());
     return PETALS_OK;
 }

@@ -556,8 +556,9 @@ def test_lm_head_backward_at_the_blocks_of_tokens(V, H, M):
 
 
 # rows that one workgroup takes as a whole: the number of rows from which on it does, both widths of workgroup, vocabularies beside them
-@pytest.mark.parametrize("V,M,K,T", [(1, 192, 1, 1.0), (7, 200, 7, 2.0), (100, 191, 100, 1.0), (1000, 193, 130, 0.5), (8193, 256, 1024, 1.0),
-                                     (65536, 192, 64, 2.0), (65537, 192, 64, 2.0), (100003, 194, 1, 1.0)])
+@pytest.mark.parametrize("V,M,K,T", [(1, 192, 1, 1.0), (7, 200, 7, 2.0), (100, 139, 100, 1.0), (300, 140, 1024, 2.0), (1000, 193, 130, 0.5),
+                                     (8193, 256, 1024, 1.0), (65536, 192, 64, 2.0), (65537, 141, 64, 2.0), (100003, 194, 1, 1.0),
+                                     (20011, 139, 1024, 1.0)])
 def test_distillation_by_whole_rows(V, M, K, T):
     c, _, _ = _client(V, 64, M)
     r, x = _logits(M, V, 31)
@@ -641,3 +642,27 @@ def test_two_clients_on_two_streams_at_once():
                 assert torch.equal(u, v), k
     for c, _, _ in calls:
         c.close()
+
+
+@pytest.mark.parametrize("V,M", [(300, 6), (50257, 6), (20011, 200)])
+@pytest.mark.parametrize("T", [1.0, 3.0])
+def test_masks_of_the_lowest_value(V, M, T):
+    """Tokens ruled out with the type's lowest number instead of an infinity, in logits and in teachers' lists."""
+    lowest = float(np.finfo(np.float32).min)
+    c, _, _ = _client(V, 64, M)
+    r, x = _logits(M, V, 36)
+    x[0] = lowest                                          # every one: all equal
+    x[1, 1:] = lowest                                      # all but the first
+    x[2, :V - 1] = lowest                                  # all but the last
+    x[3, r.random(V) < 0.9] = lowest
+    x[4, :V // 2] = lowest
+    tokens = np.full(M, V - 1, np.int32)
+    tokens[1], tokens[3] = 0, int(x[3].argmax())
+    _check_logprobs(c, x, tokens, T, 5)
+    ids = np.stack([r.permutation(np.flatnonzero(x[t] > lowest) if t else V)[:1].repeat(4) for t in range(M)]).astype(np.int32)
+    ids[5:] = r.integers(0, V, (M - 5, 4))
+    vals = r.standard_normal((M, 4)).astype(np.float32)
+    vals[:, 1] = lowest
+    vals[3] = lowest                                       # (a list of equal logits)
+    _check_distill(c, x, ids, vals, T, None)
+    c.close()
