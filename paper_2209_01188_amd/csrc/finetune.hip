@@ -19,7 +19,7 @@ namespace {
 // nearly everything: log S and -D / S are the two parts of the entropy, both >= 0, and nothing cancels between them.
 //
 // Bound by the bytes of the logits where there are many rows: 1024 x 250880 with the 20 best of each in 189 us, 5.4 TB/s (a copy
-// within the memory reaches 4.8); with few rows by the latency of two launches, 1 x 250880 in 13 us with 5 of them, in 20 with 50.
+// within the memory reaches 4.8); with few rows by the latency of two launches, 1 x 250880 in 13 us with 5 of them, in 18 with 50.
 constexpr double LN2 = 0.69314718055994530942, LOG2E = 1.4426950408889634074;
 
 struct RowStat {
@@ -80,7 +80,7 @@ constexpr int ROW_NT = 256, ROW_NW = ROW_NT / 64;   // threads of a workgroup th
 constexpr int ROW_PER = 16;                         // logits of a thread per step
 constexpr int WAVE_STEP = 64 * ROW_PER, ROW_STEP = ROW_NW * WAVE_STEP;
 // Workgroups that a call is cut into at least, if it has the steps: 4 and 8 per compute unit.  (Log probabilities of 1024 x 250880
-// with 1024, 1536: 188, 205 us, each split starts a list of its own.)
+// with 1024, 1536: 188, 205 us, each split starts a list of its own; distillation of 128 x 250880 with 1024, 2048: 74, 73.)
 constexpr int LOGPROBS_GROUPS = 1024, DISTILL_GROUPS = 2048;
 constexpr int MAX_GRID = 1 << 14;                   // rows of a launch
 typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));     // rows of an odd vocabulary begin anywhere
@@ -244,6 +244,7 @@ __device__ __forceinline__ void logprobs_store(const LogprobsOut &o, int t, int 
         o.top_logprob[(size_t)t * top_k + threadIdx.x] = none ? -INFINITY : (float)(((double)key_value(top[threadIdx.x]) - s.m) * invT - lse);
     }
 }
+
 // workgroup (split, row): the split's part of the row, and with one split the results
 __global__ void __launch_bounds__(ROW_NT) k_logprobs(LogprobsOut o, int V, int range, double invT, int top_k, RowStat *__restrict__ stats,
                                                      uint64_t *__restrict__ tops) {
