@@ -355,7 +355,7 @@ struct DistillPart {                   // of a row and split
     float m;
     double S;
 };
-struct DistillRow {                    // of a row, by the workgroup of its first split
+struct DistillRow {                    // of a row, from its list
     double max, norm;                  // of the teacher's logits, and 1 / sum of e^((logit - max) / T)
     double term, mass;                 // sum p (log p - (z - ref) / T) and sum p: with log q = z / T - lse the loss is T^2 (term + mass (lse - ref / T))
     double ref;                        // the list's largest z, so that large logits cancel exactly
